@@ -262,6 +262,45 @@ bcq_status bcq_alpha_pack(long long count, int nseg, const long long* seg_begin,
 bcq_status bcq_alpha_unpack(long long count, int nseg, const long long* seg_begin, const long long* seg_prefix,
                             const float* packed, float* alpha_flat, void* stream);
 
+/* ------------------------------------------------------------------ logits: answers and losses
+ *
+ * Operators over n rows of `vocab` logits, dtype BCQ_F32 or BCQ_BF16, row pitch ld >= vocab elements.  Rows may start at
+ * any element (no alignment beyond that of an element).  n = 0 is allowed and launches nothing; vocab <= 393216 and
+ * lists of up to 128 tokens are covered (BCQ_ERR_UNSUPPORTED otherwise); 1e-3 <= temperature <= 1e3 (BCQ_ERR_SHAPE).
+ * Logits of -inf are tokens that cannot occur.  A row that has a NaN or +inf, or nothing above -inf, is no
+ * distribution: its results are NaN (indices -1).  Sums are kept in fp32 relative to the row's maximum and joined in a
+ * fixed order, so a call gives the same result in every run. */
+
+/* Of every row x, with l = log sum_j exp(x_j / temperature):
+ *   logprob     out: float [n], x[target] / temperature - l; 0 for a negative target (no token), NaN for one >= vocab.
+ *                    targets: int64 [n].  Both or neither may be NULL
+ *   entropy     out: float [n], -sum_j p_j log p_j; may be NULL
+ *   top_logprob out: float [n][top_k], top_index out: int32 [n][top_k]: the top_k likeliest tokens in order, ties to the lowest
+ *                    index; places that no token above -inf takes hold -inf and -1.  0 <= top_k <= 128; with 0 both may be NULL */
+bcq_status bcq_token_logprobs(int n, int vocab, const void* logits, size_t ld, int dtype, const long long* targets,
+                              int top_k, float temperature, float* logprob, float* entropy, float* top_logprob,
+                              int* top_index, void* stream);
+
+/* Distillation from a teacher's top log probabilities (as bcq_token_logprobs writes them at the same temperature):
+ * top_index int32 [n][k], top_logprob float [n][k], 1 <= k <= 128, p = exp(top_logprob); entries with a negative index are
+ * left out, one >= vocab makes the row's results NaN, an index that is there twice has the sum of its p.  q is the
+ * student's distribution, softmax(x / temperature).
+ *   tail = 0: p is normalised to 1 (a row without entries has loss 0);
+ *             loss = sum_i p_i (log p_i - log q_i).  k = 1 and a log probability of 0: cross entropy with a label
+ *   tail = 1: all other tokens are one class, with r = max(0, 1 - sum p) at the teacher and rho at the student;
+ *             loss = sum_i p_i (log p_i - log q_i) + r (log r - log rho).  Where there is no other token above -inf, r counts as 0
+ * loss out: float [n] (what the terms add up to is computed in fp64: near the minimum they cancel). */
+bcq_status bcq_distill_loss(int n, int vocab, int k, const void* logits, size_t ld, int dtype, const int* top_index,
+                            const float* top_logprob, float temperature, int tail, float* loss, void* stream);
+
+/* The loss (may be NULL) and its gradient with respect to the logits, reading these once:
+ *   dlogits[t][j] = dloss[t] d loss[t] / d x[t][j]   (d / dx of x / temperature included, no other factor)
+ * dloss: float [n]; a row with dloss 0 gets zeros whatever its logits hold.  dlogits: dtype [n][lddl], lddl >= vocab; it may be
+ * `logits` itself (then lddl = ld), but may not overlap it otherwise.  Elements behind a row's last are left as they are. */
+bcq_status bcq_distill_grad(int n, int vocab, int k, const void* logits, size_t ld, int dtype, const int* top_index,
+                            const float* top_logprob, float temperature, int tail, const float* dloss, float* loss,
+                            void* dlogits, size_t lddl, void* stream);
+
 /* ------------------------------------------------------------------ status */
 
 const char* bcq_status_string(int status);

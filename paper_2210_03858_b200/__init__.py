@@ -27,7 +27,8 @@ SYMBOLS = ("bcq_pitch_words", "bcq_bits_bytes", "bcq_num_groups", "bcq_alpha_cou
            "bcq_kernel_launches", "bcq_linear_decode_noalloc", "bcq_decode_pack_bytes",
            "bcq_decode_pack", "bcq_linear_decode_packed", "bcq_lr_linear_decay", "bcq_alpha_adamw",
            "bcq_alpha_pack", "bcq_alpha_unpack", "bcq_prepared_bytes", "bcq_prepare_planes",
-           "bcq_linear_fwd_prepared", "bcq_linear_bwd_x_prepared", "bcq_check_device")
+           "bcq_linear_fwd_prepared", "bcq_linear_bwd_x_prepared", "bcq_check_device", "bcq_token_logprobs",
+           "bcq_distill_loss", "bcq_distill_grad")
 
 
 class BcqError(RuntimeError):
@@ -98,6 +99,12 @@ def lib() -> C.CDLL:
         l.bcq_alpha_unpack.argtypes = [ll, i, vp, vp, vp, vp, vp]
         l.bcq_linear_bwd_alpha.restype = i
         l.bcq_linear_bwd_alpha.argtypes = [i, i, i, i, i, vp, sz, vp, sz, vp, u32, f32, i, vp, vp, sz, vp]
+        l.bcq_token_logprobs.restype = i
+        l.bcq_token_logprobs.argtypes = [i, i, vp, sz, i, vp, i, f32, vp, vp, vp, vp, vp]
+        l.bcq_distill_loss.restype = i
+        l.bcq_distill_loss.argtypes = [i, i, i, vp, sz, i, vp, vp, f32, i, vp, vp]
+        l.bcq_distill_grad.restype = i
+        l.bcq_distill_grad.argtypes = [i, i, i, vp, sz, i, vp, vp, f32, i, vp, vp, vp, sz, vp]
         l.bcq_status_string.restype = C.c_char_p
         l.bcq_status_string.argtypes = [i]
         l.bcq_last_cuda_error.restype = i
@@ -441,6 +448,91 @@ def alpha_unpack(packed, alpha_flat, segments: Segments):
     assert packed.numel() == segments.count
     _check(_fn().unpack(segments.count, segments.nseg, _ptr(segments.begin), _ptr(segments.prefix),
                                   _ptr(packed), _ptr(alpha_flat), _stream()), "bcq_alpha_unpack")
+
+
+# ---------------------------------------------------------------------------- logits: answers and losses
+
+def _device_of(name, t, dtype=None, shape=None):
+    """Checks an operand: on the current device (the stream is that device's), of the type and shape given, dense."""
+    torch = _torch()
+    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError("%s must be on the current CUDA device" % name)
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError("%s must be %s" % (name, dtype))
+    if shape is not None and (tuple(t.shape) != shape or not t.is_contiguous()):
+        raise ValueError("%s must be contiguous, of shape %s" % (name, list(shape)))
+
+
+def _rows(name, t):
+    """(rows, columns, row pitch) of a matrix whose rows are dense."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must have two dimensions and dense rows" % name)
+    n, cols = t.shape
+    return n, cols, t.stride(0) if n > 1 else max(cols, t.stride(0))
+
+
+def token_logprobs(logits, targets=None, top_k: int = 0, temperature: float = 1.0):
+    """bcq_token_logprobs: logits bf16 or fp32 [n][vocab], targets int64 [n] or None -> (logprob fp32 [n] or None, entropy
+    fp32 [n], top_logprob fp32 [n][top_k], top_index int32 [n][top_k]) of softmax(logits / temperature)."""
+    torch = _torch()
+    _device_of("logits", logits)
+    n, vocab, ld = _rows("logits", logits)
+    dtype = _dtype_code(logits)
+    if targets is not None:
+        _device_of("targets", targets, torch.int64, (n,))
+    k = max(0, top_k)
+    logprob = None if targets is None else _empty(logits, (n,), torch.float32)
+    entropy = _empty(logits, (n,), torch.float32)
+    top, index = _empty(logits, (n, k), torch.float32), _empty(logits, (n, k), torch.int32)
+    _check(_fn().token_logprobs(n, vocab, _ptr(logits), ld, dtype, _ptr(targets), top_k, temperature, _ptr(logprob),
+                                _ptr(entropy), _ptr(top) if k else None, _ptr(index) if k else None, _stream()),
+           "bcq_token_logprobs")
+    return logprob, entropy, top, index
+
+
+def _teacher(n, top_index, top_logprob):
+    torch = _torch()
+    if top_index.dim() != 2:
+        raise ValueError("top_index must have two dimensions")
+    k = top_index.shape[1]
+    _device_of("top_index", top_index, torch.int32, (n, k))
+    _device_of("top_logprob", top_logprob, torch.float32, (n, k))
+    return k
+
+
+def distill_loss(logits, top_index, top_logprob, temperature: float = 1.0, tail: bool = True):
+    """bcq_distill_loss: student logits bf16 or fp32 [n][vocab], the teacher's top_index int32 and top_logprob fp32 [n][k] (as
+    token_logprobs gives them at the same temperature) -> loss fp32 [n]."""
+    torch = _torch()
+    _device_of("logits", logits)
+    n, vocab, ld = _rows("logits", logits)
+    k = _teacher(n, top_index, top_logprob)
+    loss = _empty(logits, (n,), torch.float32)
+    _check(_fn().distill_loss(n, vocab, k, _ptr(logits), ld, _dtype_code(logits), _ptr(top_index), _ptr(top_logprob), temperature,
+                              1 if tail else 0, _ptr(loss), _stream()), "bcq_distill_loss")
+    return loss
+
+
+def distill_grad(logits, top_index, top_logprob, dloss, temperature: float = 1.0, tail: bool = True, out=None):
+    """bcq_distill_grad: as distill_loss, with dloss fp32 [n] (what the loss of each row counts) -> (loss fp32 [n], dlogits
+    [n][vocab] in the type of the logits).  ``out`` may be the logits themselves.  dlogits created here is a view whose rows are
+    16-byte aligned, so a bf16 one is a dY for linear_bwd_x and linear_bwd_alpha."""
+    torch = _torch()
+    _device_of("logits", logits)
+    n, vocab, ld = _rows("logits", logits)
+    k = _teacher(n, top_index, top_logprob)
+    _device_of("dloss", dloss, torch.float32, (n,))
+    dtype = _dtype_code(logits)
+    if out is None:
+        out = _empty(logits, (n, -(-vocab // 8) * 8), logits.dtype)[:, :vocab]
+    _device_of("out", out, logits.dtype)
+    if out.shape != logits.shape:
+        raise ValueError("out must have the shape of the logits")
+    _, _, ldd = _rows("out", out)
+    loss = _empty(logits, (n,), torch.float32)
+    _check(_fn().distill_grad(n, vocab, k, _ptr(logits), ld, dtype, _ptr(top_index), _ptr(top_logprob), temperature, 1 if tail else 0,
+                              _ptr(dloss), _ptr(loss), _ptr(out), ldd, _stream()), "bcq_distill_grad")
+    return loss, out
 
 
 def kernel_launches() -> int:

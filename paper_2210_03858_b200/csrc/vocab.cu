@@ -1,0 +1,1068 @@
+// Operators over rows of logits: log probabilities of given tokens with entropy and top alternatives, and the
+// distillation loss against a teacher's top log probabilities with its gradient.
+//
+// With c = log2(e) / T everything is a sum over a row of 2^(c (x - m)), m = max x.  All three kernels read a row once
+// from memory: a thread keeps a running maximum and the sums that go with it, and rescales them when a batch of its
+// vectors has a larger one, so no second pass is needed for the sums; the sums of threads, warps and CTAs are joined in
+// a fixed order.  The difference is taken before it is scaled: c x alone overflows for a logit of the type's
+// lowest value, and a row that holds nothing else is a row of equals.  What bounds them is memory: n vocab sizeof(T) bytes read (and written, for the
+// gradient).  An element costs one exponential, two packed half-instructions and a conversion; the exponentials
+// alone (16 a cycle and SM) take 0.7 of the time the bytes of bf16 logits take, so whatever else an element costs has to
+// issue beside them: sums and products go two at a time (fma.rn.f32x2), maxima of bf16 two at a time, and the
+// comparison that guards the running maximum is made once for a batch of four vectors.
+//
+// Rows start at any element (an odd vocabulary in bf16 leaves rows at odd addresses): the elements before the
+// first and after the last whole 16-byte vector of a row belong to single threads.
+//
+// A row goes to a cluster of 1, 2, 4 or 8 CTAs, more where there are few rows: one row of 50257 elements is 100 KB, which
+// one SM alone takes 3 us to bring in.
+#include <cuda_bf16.h>
+
+#include <algorithm>
+
+#include "gemm_common.cuh"
+
+namespace {
+
+using namespace bcq;
+
+constexpr int kVocabMax = 393216;
+constexpr int kTopMax = 128;
+constexpr int kBatch = 4;          // 16-byte vectors of a thread between two looks at the running maximum
+constexpr float kFloor = -1000.0f; // exponents below are as good as this one (2^-1000 = 0), and 0 * -1000 is 0
+constexpr int kCandidates = 2048;  // elements, and batches, that may be as large as the k-th largest
+constexpr float kLn2 = 0.693147180559945309f;
+
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
+__device__ __forceinline__ float quiet_nan() { return __int_as_float(0x7fc00000); }
+
+// Two floats in a register pair: what the packed instructions of sm_100 take.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float a, float b) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// ---------------------------------------------------------------- element types
+
+template <typename T>
+struct Elem;
+template <>
+struct Elem<float> {
+    static constexpr int E = 4;  // of a 16-byte vector
+    static constexpr uint32_t kMasked = 0xff800000u;
+    static __device__ __forceinline__ float get(const float* p) { return ld(p); }
+    static __device__ __forceinline__ float at(const uint4& v, int i) {
+        return __uint_as_float(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w);
+    }
+    static __device__ __forceinline__ float max_of(const uint4& v) {
+        return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)), max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
+    }
+    static __device__ __forceinline__ float max_of4(const uint4* v) {
+        return max_nan(max_nan(max_of(v[0]), max_of(v[1])), max_nan(max_of(v[2]), max_of(v[3])));
+    }
+    static __device__ __forceinline__ void pairs(const uint4& v, f32x2* x) {
+        x[0] = pack2(__uint_as_float(v.x), __uint_as_float(v.y));
+        x[1] = pack2(__uint_as_float(v.z), __uint_as_float(v.w));
+    }
+    static __device__ __forceinline__ void mask(uint4& v, uint32_t bits) {
+        if (bits & 1u) v.x = kMasked;
+        if (bits & 2u) v.y = kMasked;
+        if (bits & 4u) v.z = kMasked;
+        if (bits & 8u) v.w = kMasked;
+    }
+};
+template <>
+struct Elem<__nv_bfloat16> {
+    static constexpr int E = 8;
+    static constexpr uint32_t kMasked = 0xff80ff80u;
+    static __device__ __forceinline__ float get(const __nv_bfloat16* p) {
+        unsigned short h;
+        asm volatile("ld.global.u16 %0, [%1];" : "=h"(h) : "l"(p));
+        return __uint_as_float((uint32_t)h << 16);
+    }
+    static __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+    static __device__ __forceinline__ float at(const uint4& v, int i) {
+        const uint32_t w = word(v, i >> 1);
+        return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+    }
+    static __device__ __forceinline__ uint32_t max2_of(const uint4& v) {
+        return max_nan_bf16x2(max_nan_bf16x2(v.x, v.y), max_nan_bf16x2(v.z, v.w));
+    }
+    static __device__ __forceinline__ float max_of4(const uint4* v) {
+        const uint32_t m = max_nan_bf16x2(max_nan_bf16x2(max2_of(v[0]), max2_of(v[1])), max_nan_bf16x2(max2_of(v[2]), max2_of(v[3])));
+        return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+    }
+    static __device__ __forceinline__ void pairs(const uint4& v, f32x2* x) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = word(v, i);
+            x[i] = pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+        }
+    }
+    static __device__ __forceinline__ void mask(uint4& v, uint32_t bits) {
+        uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (bits & (1u << (2 * i))) w[i] = (w[i] & 0xffff0000u) | 0xff80u;
+            if (bits & (2u << (2 * i))) w[i] = (w[i] & 0x0000ffffu) | 0xff800000u;
+        }
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+
+// The elements of a row that a CTA of its cluster has: whole vectors [v0, v1), and single elements at the ends of the row,
+// one to a thread (element -1: none).
+template <typename T>
+struct Share {
+    const T* row;
+    int head;          // elements before the first whole vector of the row
+    int v0, v1, nvec;  // vectors of this CTA, and of the row
+    int single;        // this thread's
+    int first, last;   // elements [first, last) of this CTA
+
+    __device__ __forceinline__ Share(const T* row_, int vocab, int rank, int ctas) : row(row_) {
+        constexpr int E = Elem<T>::E;
+        head = min(vocab, (int)(((16u - (uint32_t)(reinterpret_cast<uintptr_t>(row_) & 15u)) & 15u) / sizeof(T)));
+        nvec = (vocab - head) / E;
+        const int per = (nvec + ctas - 1) / ctas;
+        v0 = min(nvec, rank * per);
+        v1 = min(nvec, v0 + per);
+        const int tail0 = head + nvec * E, tid = (int)threadIdx.x;
+        single = -1;
+        if (rank == 0 && tid < head) single = tid;
+        if (rank == ctas - 1 && tid >= E && tid < E + (vocab - tail0)) single = tail0 + tid - E;  // (head < E)
+        first = rank == 0 ? 0 : head + v0 * E;
+        last = rank == ctas - 1 ? vocab : head + v1 * E;
+    }
+    __device__ __forceinline__ const uint4* vec(int v) const { return reinterpret_cast<const uint4*>(row + head) + v; }
+};
+
+// Running maximum and the sums relative to it.  ENTROPY: sum of e z too, z the exponent of e.
+template <typename T, bool ENTROPY>
+struct Running {
+    float m = neg_inf();
+    f32x2 s = 0, t = 0;  // (two partial sums each)
+    bool bad = false;    // a NaN or +inf was seen
+
+    __device__ __forceinline__ void raise(float x, float c) {
+        if (x > m) {
+            const float d = fmaxf((m - x) * c, kFloor), f = ex2(d);
+            const f32x2 ff = pack2(f, f);
+            if (ENTROPY) t = mul2(ff, fma2(pack2(d, d), s, t));
+            s = mul2(ff, s);
+            m = x;
+        }
+        if (!(x < __int_as_float(0x7f800000))) bad = true;
+    }
+    __device__ __forceinline__ float base() const { return m == neg_inf() ? 0.0f : m; }
+    __device__ __forceinline__ void add(const uint4& v, f32x2 c2, f32x2 nm2) {
+        f32x2 x[Elem<T>::E / 2];
+        Elem<T>::pairs(v, x);
+#pragma unroll
+        for (int i = 0; i < Elem<T>::E / 2; ++i) {
+            float a, b;
+            unpack2(mul2(add2(x[i], nm2), c2), a, b);
+            if (ENTROPY) {
+                a = fmaxf(a, kFloor);
+                b = fmaxf(b, kFloor);
+            }
+            const f32x2 e = pack2(ex2(a), ex2(b));
+            s = add2(s, e);
+            if (ENTROPY) t = fma2(e, pack2(a, b), t);
+        }
+    }
+    __device__ __forceinline__ float batch(const uint4 (&v)[kBatch], float c) {
+        const float x = Elem<T>::max_of4(v);
+        raise(x, c);
+        const float b = -base();
+        const f32x2 c2 = pack2(c, c), nm2 = pack2(b, b);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) add(v[u], c2, nm2);
+        return x;
+    }
+    __device__ __forceinline__ void one(float x, float c) {
+        raise(x, c);
+        const float z = fmaxf((x - base()) * c, kFloor), e = ex2(z);
+        s = add2(s, pack2(e, 0.0f));
+        if (ENTROPY) t = fma2(pack2(e, 0.0f), pack2(z, 0.0f), t);
+    }
+    __device__ __forceinline__ void sums(float& s1, float& t1) const {
+        float a, b;
+        unpack2(s, a, b);
+        s1 = a + b;
+        unpack2(t, a, b);
+        t1 = a + b;
+    }
+};
+
+struct Stats {
+    float m, s, t;
+    int bad;
+};
+
+// Takes two sums over different elements to the larger of their maxima.
+__device__ __forceinline__ Stats join(const Stats& a, const Stats& b, float c) {
+    Stats r;
+    r.m = fmaxf(a.m, b.m);
+    const float base = r.m == neg_inf() ? 0.0f : r.m;
+    const float da = fmaxf((a.m - base) * c, kFloor), db = fmaxf((b.m - base) * c, kFloor), fa = ex2(da), fb = ex2(db);
+    r.s = a.s * fa + b.s * fb;
+    r.t = fa * (a.t + da * a.s) + fb * (b.t + db * b.s);
+    r.bad = a.bad | b.bad;
+    return r;
+}
+
+__device__ __forceinline__ Stats join_warp(Stats v, float c) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        Stats w;
+        w.m = __shfl_xor_sync(0xffffffffu, v.m, o);
+        w.s = __shfl_xor_sync(0xffffffffu, v.s, o);
+        w.t = __shfl_xor_sync(0xffffffffu, v.t, o);
+        w.bad = __shfl_xor_sync(0xffffffffu, v.bad, o);
+        v = join(v, w, c);
+    }
+    return v;
+}
+
+// Everything of the row, in every thread of the cluster.  `warps` holds NT / 32 entries; `mine` is read by the other CTAs.
+template <int NT>
+__device__ __forceinline__ Stats join_row(Stats v, Stats* warps, Stats* mine, int ctas, float c) {
+    v = join_warp(v, c);
+    if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = warps[0];
+#pragma unroll
+    for (int w = 1; w < NT / 32; ++w) v = join(v, warps[w], c);
+    if (ctas == 1) return v;
+    if (threadIdx.x == 0) *mine = v;
+    __syncwarp();
+    ptx::cluster_sync();
+    static_assert(sizeof(Stats) == 16, "one load");
+    for (int r = 0; r < ctas; ++r) {
+        const float4 f = ptx::ld_cluster_v4(ptx::cluster_addr(ptx::smem_u32(mine), (uint32_t)r));
+        const Stats w = {f.x, f.y, f.z, __float_as_int(f.w)};
+        v = r == 0 ? w : join(v, w, c);
+    }
+    return v;
+}
+
+// Order of the top list: larger value first, then the lower index.  Zeros of either sign are equal.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    const uint32_t b = __float_as_uint(x + 0.0f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
+__device__ __forceinline__ unsigned long long key_of(float x, int index) {
+    return ((unsigned long long)order_of(x) << 32) | (uint32_t)~index;
+}
+
+// ---------------------------------------------------------------- log probabilities
+
+constexpr int kLpThreads = 256;
+
+struct TopShared {
+    unsigned long long cand[kCandidates];
+    unsigned long long best[kTopMax];       // of this CTA, in order; 0: none
+    unsigned long long others[8 * kTopMax]; // the lists of the cluster
+    float largest[kLpThreads];              // of each thread
+    int events[kCandidates];
+    int num_cand, num_events;
+    float threshold;
+    unsigned long long sum;
+};
+
+template <int NT>
+__device__ unsigned long long block_sum(unsigned long long v, unsigned long long* cell) {
+    if (threadIdx.x == 0) *cell = 0;
+    __syncthreads();
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) == 0) atomicAdd(cell, v);  // (whole numbers: any order)
+    __syncthreads();
+    v = *cell;
+    __syncthreads();
+    return v;
+}
+
+// More elements than fit are as large as the lower bound (long runs of equal logits): the k-th largest value by bisection over
+// the order of values, then the index up to which elements of that value belong to the list.  Every step reads this
+// CTA's share of the row again.
+template <typename T>
+__device__ __noinline__ void gather_exactly(const Share<T> sh, int k, TopShared* ts) {
+    constexpr int E = Elem<T>::E, NT = kLpThreads;
+    auto each = [&](auto f) {
+        for (int v = sh.v0 + (int)threadIdx.x; v < sh.v1; v += NT) {
+            const uint4 x = ld(sh.vec(v));
+            for (int i = 0; i < E; ++i) f(order_of(Elem<T>::at(x, i)), sh.head + v * E + i);
+        }
+        if (sh.single >= 0) f(order_of(Elem<T>::get(sh.row + sh.single)), sh.single);
+    };
+    auto count = [&](auto f) {
+        unsigned long long c = 0;
+        each([&](uint32_t o, int i) { c += f(o, i) ? 1 : 0; });
+        return block_sum<NT>(c, &ts->sum);
+    };
+    uint32_t lo = order_of(neg_inf()) + 1, hi = order_of(__int_as_float(0x7f7fffff));  // the k-th largest is in [lo, hi]
+    while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo + 1) / 2;
+        if (count([&](uint32_t o, int) { return o >= mid; }) >= (unsigned long long)k) lo = mid;
+        else hi = mid - 1;
+    }
+    const uint32_t kth = lo;
+    const unsigned long long above = count([&](uint32_t o, int) { return o > kth; });
+    int a = 0, b = sh.last - 1;  // the last index that still belongs is in [a, b]
+    while (a < b) {
+        const int mid = a + (b - a) / 2;
+        if (above + count([&](uint32_t o, int i) { return o == kth && i <= mid; }) >= (unsigned long long)k) b = mid;
+        else a = mid + 1;
+    }
+    if (threadIdx.x == 0) ts->num_cand = 0;
+    __syncthreads();
+    each([&](uint32_t o, int i) {
+        if (o > kth || (o == kth && i <= a)) {
+            const int at = atomicAdd(&ts->num_cand, 1);
+            if (at < kCandidates) ts->cand[at] = ((unsigned long long)o << 32) | (uint32_t)~i;  // (k of them)
+        }
+    });
+    __syncthreads();
+}
+
+// The k largest of this CTA's share, in order, to ts->best.  k distinct threads have an element at least as large as the
+// k-th largest of the threads' maxima, so that is a lower bound of the k-th largest element, and only batches
+// whose maximum reaches it are read again (with 50257 elements and k = 64 about 75 batches and as many elements).
+template <typename T>
+__device__ __forceinline__ void top_of_share(const Share<T>& sh, int k, float mine, float single, const float* batch_max, int batches,
+                                             TopShared* ts) {
+    constexpr int E = Elem<T>::E, NT = kLpThreads;
+    const int tid = (int)threadIdx.x;
+    ts->largest[tid] = mine;
+    if (tid == 0) {
+        ts->num_cand = 0;
+        ts->num_events = 0;
+    }
+    __syncthreads();
+    int rank = 0;
+    for (int i = 0; i < NT; i += 4) {
+        const float4 o = *reinterpret_cast<const float4*>(&ts->largest[i]);
+        rank += (o.x > mine || (o.x == mine && i < tid)) + (o.y > mine || (o.y == mine && i + 1 < tid)) +
+                (o.z > mine || (o.z == mine && i + 2 < tid)) + (o.w > mine || (o.w == mine && i + 3 < tid));
+    }
+    if (rank == k - 1) ts->threshold = mine;
+    for (int i = tid; i < k; i += NT) ts->best[i] = 0;
+    __syncthreads();
+    const float bound = ts->threshold;
+    auto belongs = [&](float x) { return x >= bound && x > neg_inf(); };
+    auto take = [&](float x, int index) {
+        const int at = atomicAdd(&ts->num_cand, 1);
+        if (at < kCandidates) ts->cand[at] = key_of(x, index);
+    };
+    if (sh.single >= 0 && belongs(single)) take(single, sh.single);
+    if (belongs(mine))
+        for (int b = 0; b < batches; ++b)
+            if (belongs(batch_max[b * NT + tid])) {
+                const int at = atomicAdd(&ts->num_events, 1);
+                if (at < kCandidates) ts->events[at] = b * NT + tid;
+            }
+    __syncthreads();
+    const int events = ts->num_events;
+    if (events <= kCandidates)
+        for (int i = tid; i < events * kBatch; i += NT) {
+            const int e = ts->events[i / kBatch];
+            const int v = sh.v0 + ((e / NT) * kBatch + i % kBatch) * NT + e % NT;
+            if (v < sh.v1) {
+                const uint4 x = ld(sh.vec(v));
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    const float y = Elem<T>::at(x, j);
+                    if (belongs(y)) take(y, sh.head + v * E + j);
+                }
+            }
+        }
+    __syncthreads();
+    if (events > kCandidates || ts->num_cand > kCandidates) gather_exactly<T>(sh, k, ts);
+    const int n = min(ts->num_cand, kCandidates);
+    for (int i = tid; i < n; i += NT) {
+        const unsigned long long key = ts->cand[i];
+        int r = 0;
+        for (int j = 0; j < n; ++j) r += ts->cand[j] > key;
+        if (r < k) ts->best[r] = key;
+    }
+    __syncthreads();
+}
+
+struct LogprobParams {
+    int vocab, ctas, top;
+    long long ld;
+    const long long* targets;
+    float c, inv_t;
+    float *logprob, *entropy, *top_logprob;
+    int* top_index;
+};
+
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(kLpThreads)
+token_logprobs_kernel(const T* logits, const LogprobParams p) {
+    constexpr int NT = kLpThreads;
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ Stats warps[NT / 32];
+    __shared__ Stats mine;
+    pdl_wait();
+    const int row = (int)blockIdx.x / p.ctas, rank = (int)blockIdx.x % p.ctas;
+    const Share<T> sh(logits + (long long)row * p.ld, p.vocab, rank, p.ctas);
+    const int tid = (int)threadIdx.x;
+    TopShared* ts = reinterpret_cast<TopShared*>(smem);
+    float* batch_max = reinterpret_cast<float*>(smem + sizeof(TopShared));
+
+    // of the given token (wanted by one thread at the end)
+    long long target = -1;
+    float given = 0.0f;
+    if (rank == 0 && tid == 0 && p.targets != nullptr) {
+        target = ld(p.targets + row);
+        if (target >= 0 && target < p.vocab) given = Elem<T>::get(sh.row + target);
+    }
+    const float single = sh.single >= 0 ? Elem<T>::get(sh.row + sh.single) : neg_inf();
+
+    Running<T, true> run;
+    const uint4 masked = make_uint4(Elem<T>::kMasked, Elem<T>::kMasked, Elem<T>::kMasked, Elem<T>::kMasked);
+    auto load = [&](int b, uint4 (&v)[kBatch]) {
+        const int at = sh.v0 + b * (kBatch * NT) + tid;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) v[u] = at + u * NT < sh.v1 ? ld_stream(sh.vec(at + u * NT)) : masked;
+    };
+    // the next batch is on its way while one is added up
+    uint4 now[kBatch], next[kBatch];
+    const int batches = (sh.v1 - sh.v0 + kBatch * NT - 1) / (kBatch * NT);
+    if (batches > 0) load(0, now);
+    for (int b = 0; b < batches; ++b) {
+        if (b + 1 < batches) load(b + 1, next);
+        const float x = run.batch(now, p.c);
+        if (TOP) batch_max[b * NT + tid] = x;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) now[u] = next[u];
+    }
+    if (sh.single >= 0) run.one(single, p.c);
+
+    Stats st;
+    run.sums(st.s, st.t);
+    st.m = run.m;
+    st.bad = run.bad ? 1 : 0;
+    st = join_row<NT>(st, warps, &mine, p.ctas, p.c);
+    const bool none = st.bad || !(st.s > 0.0f);  // no distribution
+    const float log_s = log2f(st.s);
+    if (rank == 0 && tid == 0) {
+        if (p.logprob != nullptr) {
+            float lp = (given - st.m) * p.inv_t - log_s * kLn2;
+            if (none || target >= p.vocab) lp = quiet_nan();
+            else if (target < 0) lp = 0.0f;
+            p.logprob[row] = lp;
+        }
+        if (p.entropy != nullptr) p.entropy[row] = none ? quiet_nan() : (log_s - st.t / st.s) * kLn2;
+    }
+    if (TOP) {
+        const int k = p.top;
+        float* out = p.top_logprob + (long long)row * k;
+        int* out_i = p.top_index + (long long)row * k;
+        auto put = [&](int at, unsigned long long key) {
+            out[at] = key ? (value_of((uint32_t)(key >> 32)) - st.m) * p.inv_t - log_s * kLn2 : neg_inf();
+            out_i[at] = key ? (int)~(uint32_t)key : -1;
+        };
+        if (none) {  // the same in all CTAs of the row
+            if (rank == 0)
+                for (int i = tid; i < k; i += NT) {
+                    out[i] = quiet_nan();
+                    out_i[i] = -1;
+                }
+        } else {
+            top_of_share<T>(sh, k, run.m, single, batch_max, batches, ts);
+            if (p.ctas == 1) {
+                for (int i = tid; i < k; i += NT) put(i, ts->best[i]);
+            } else {
+                // each CTA finds the places of its own in the row's list: those of the other lists that come before, by
+                // bisection in copies of them
+                __syncwarp();
+                ptx::cluster_sync();
+                for (int i = tid; i < p.ctas * k; i += NT) {
+                    unsigned long long key;
+                    const uint32_t from = ptx::cluster_addr(ptx::smem_u32(&ts->best[i % k]), (uint32_t)(i / k));
+                    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(key) : "r"(from) : "memory");
+                    ts->others[i] = key;
+                }
+                __syncthreads();
+                for (int i = tid; i < k; i += NT) {
+                    const unsigned long long key = ts->best[i];
+                    if (key == 0) continue;
+                    int place = i;
+                    for (int r = 0; r < p.ctas; ++r) {
+                        if (r == rank) continue;
+                        const unsigned long long* list = ts->others + r * k;
+                        int lo = 0, hi = k;  // how many are larger
+                        while (lo < hi) {
+                            const int mid = (lo + hi) >> 1;
+                            if (list[mid] > key) lo = mid + 1;
+                            else hi = mid;
+                        }
+                        place += lo;
+                    }
+                    if (place < k) put(place, key);
+                }
+                // places that no element takes
+                if (rank == 0) {
+                    int have = 0;
+                    for (int r = 0; r < p.ctas; ++r) {
+                        const unsigned long long* list = ts->others + r * k;
+                        int lo = 0, hi = k;
+                        while (lo < hi) {
+                            const int mid = (lo + hi) >> 1;
+                            if (list[mid] != 0) lo = mid + 1;
+                            else hi = mid;
+                        }
+                        have += lo;
+                    }
+                    for (int i = tid; i < k; i += NT)
+                        if (i >= have) put(i, 0);
+                }
+            }
+        }
+    }
+    __syncwarp();
+    if (p.ctas > 1) ptx::cluster_sync();  // nobody's memory goes away while it is read
+}
+
+// ---------------------------------------------------------------- distillation
+
+// The teacher's tokens of a row.
+struct Teacher {
+    int index[kTopMax];   // -1: left out
+    float logp[kTopMax];
+    float x[kTopMax];     // the student's logit of the token
+    double p[kTopMax];
+    int first[kTopMax];   // 1: the first entry with this index
+    int repeated;         // some index is there twice
+    int bad;
+    double total;         // of p
+    // from the whole row
+    int none;             // no distribution
+    float m, s;           // the largest logit, the sum over all tokens
+    float m_rest, s_rest; // the same of the tokens that the teacher does not name (0 and 0: there is none)
+    float scale_rest, scale_own;  // of 2^(c (x - m_rest)) and 2^(c (x - m)) in the gradient
+};
+
+struct DistillParams {
+    int vocab, ctas, k, tail;
+    long long ld, ldd;
+    const int* index;
+    const float* logp;
+    const float* dloss;
+    float c, inv_t;
+    double inv_t64;
+    float* loss;
+};
+
+__device__ __forceinline__ double warp_sum(double v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// Loads the teacher's list and marks its tokens among this CTA's vectors: bit i of marks[v - v0 + 1] is element i of vector v, the
+// bytes at both ends stand for the single elements before and after the vectors.
+template <typename T, int NT>
+__device__ __forceinline__ void load_teacher(const Share<T>& sh, const DistillParams& p, int row, Teacher* te, uint32_t* marks) {
+    constexpr int E = Elem<T>::E;
+    const int tid = (int)threadIdx.x;
+    int index = -1;
+    float lp = 0.0f;
+    bool bad = false;
+    if (tid < p.k) {
+        index = ld(p.index + (long long)row * p.k + tid);
+        lp = ld(p.logp + (long long)row * p.k + tid);
+        if (index >= p.vocab) bad = true;
+        if (index < 0 || bad) index = -1;
+    }
+    const int words = (sh.v1 - sh.v0 + 2 + 3) / 4;
+    for (int i = tid; i < words; i += NT) marks[i] = 0;
+    if (tid == 0) {
+        te->repeated = p.ctas > 1;  // (a CTA sees repetitions among its own elements only)
+        te->bad = 0;
+    }
+    __syncthreads();
+    if (tid < p.k) {
+        te->index[tid] = index;
+        te->logp[tid] = lp;
+        te->first[tid] = index >= 0;
+        te->p[tid] = index >= 0 ? exp((double)lp) : 0.0;
+        const float x = index >= 0 ? Elem<T>::get(sh.row + index) : neg_inf();
+        te->x[tid] = x;
+        if (bad || !(x < __int_as_float(0x7f800000))) te->bad = 1;
+        if (index >= sh.first && index < sh.last) {
+            const int at = index - (sh.head + sh.v0 * E) + E;  // >= 0: the elements before the first vector are fewer than E
+            const int byte = at / E;
+            const uint32_t bit = 1u << (8 * (byte & 3) + at % E);
+            if (atomicOr(&marks[byte >> 2], bit) & bit) te->repeated = 1;
+        }
+    }
+    __syncthreads();
+    if (te->repeated && tid < p.k && index >= 0) {
+        bool seen = false;
+        for (int i = 0; i < tid; ++i) seen |= te->index[i] == index;
+        te->first[tid] = !seen;
+    }
+    if (tid >= 32 && tid < 64) {
+        double total = 0.0;
+        for (int i = tid - 32; i < p.k; i += 32) total += te->p[i];
+        total = warp_sum(total);
+        if (tid == 32) te->total = total;
+    }
+    // (first and total are read after the barriers of join_row)
+}
+
+// What a class adds to the divergence, p (d + expm1(-d)) with d = log p - log q: never negative, so near distributions lose
+// nothing to the cancellation of p log p against p log q, and a common error of all log q (that of the row's sum) drops
+// out.  In 64 bits: k + 1 values a row.
+__device__ __forceinline__ double class_loss(double p, double log_p, double log_q) {
+    if (!(p > 0.0)) return p == 0.0 ? exp(log_q) : p;
+    const double d = log_p - log_q;
+    return p * (d + expm1(-d));
+}
+
+// What P, r and rho are: p sums up to `keep` without a tail.
+struct Masses {
+    double keep, mass, r;
+};
+__device__ __forceinline__ Masses masses(const DistillParams& p, const Teacher* te) {
+    Masses v;
+    const double total = te->total;
+    v.keep = p.tail ? 1.0 : (total > 0.0 ? 1.0 / total : 0.0);
+    v.mass = p.tail ? total : (total == 0.0 ? 0.0 : total * v.keep);
+    v.r = p.tail && te->s_rest > 0.0f ? fmax(0.0, 1.0 - v.mass) : 0.0;
+    return v;
+}
+
+// The row's sums with the teacher's tokens, and the factors of its gradient, from the sum over all other tokens.  One warp.
+__device__ __forceinline__ void finish_row(const DistillParams& p, Teacher* te, const Stats& rest, float w) {
+    const int lane = (int)threadIdx.x & 31;
+    float m = rest.m;
+    for (int i = lane; i < p.k; i += 32)
+        if (te->first[i]) m = fmaxf(m, te->x[i]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (m == neg_inf()) m = 0.0f;
+    float s = 0.0f;
+    for (int i = lane; i < p.k; i += 32)
+        if (te->first[i]) s += ex2(fmaxf((te->x[i] - m) * p.c, kFloor));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane == 0) {
+        // The rest keeps its own maximum: rho may be too small for a float where its logarithm, and the shares of its
+        // tokens in it, are not.
+        const float down = ex2(fmaxf((rest.m - m) * p.c, kFloor));
+        te->m_rest = rest.m == neg_inf() ? 0.0f : rest.m;
+        te->s_rest = rest.s;
+        te->m = m;
+        te->s = s + rest.s * down;
+        te->none = rest.bad || te->bad || !(te->s > 0.0f);
+        const Masses v = masses(p, te);
+        const float f = w * p.inv_t, mass = (float)(v.mass + v.r);
+        te->scale_own = f * mass / te->s;
+        te->scale_rest = f * (mass * (down / te->s) - (v.r > 0.0 ? (float)v.r / rest.s : 0.0f));
+    }
+}
+
+// Loss of the row.  One warp, after finish_row.
+__device__ __forceinline__ float loss_of_row(const DistillParams& p, const Teacher* te) {
+    const int lane = (int)threadIdx.x & 31;
+    const Masses v = masses(p, te);
+    const double log_s = log((double)te->s), log_keep = p.tail || v.mass == 0.0 ? 0.0 : log(v.keep);
+    double loss = 0.0;
+    for (int i = lane; i < p.k; i += 32) {
+        if (te->index[i] < 0) continue;
+        const double log_q = ((double)te->x[i] - (double)te->m) * p.inv_t64 - log_s;
+        loss += class_loss(te->p[i] * v.keep, (double)te->logp[i] + log_keep, log_q);
+        if (!te->first[i]) loss -= exp(log_q);  // its q counts once
+    }
+    loss = warp_sum(loss);
+    const double log_rho = ((double)te->m_rest - (double)te->m) * p.inv_t64 + log((double)te->s_rest) - log_s;
+    loss += class_loss(v.r, log(v.r), log_rho) + (v.mass + v.r - 1.0);
+    if (v.mass == 0.0 && v.r == 0.0) loss = 0.0;  // the teacher says nothing
+    return te->none ? quiet_nan() : (float)loss;
+}
+
+constexpr int kLossThreads = 256;
+
+template <typename T>
+__global__ void __launch_bounds__(kLossThreads)
+distill_loss_kernel(const T* logits, const DistillParams p) {
+    constexpr int NT = kLossThreads;
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ Stats warps[NT / 32];
+    __shared__ Stats mine;
+    __shared__ Teacher te;
+    uint32_t* marks = reinterpret_cast<uint32_t*>(smem);
+    pdl_wait();
+    const int row = (int)blockIdx.x / p.ctas, rank = (int)blockIdx.x % p.ctas;
+    const Share<T> sh(logits + (long long)row * p.ld, p.vocab, rank, p.ctas);
+    const int tid = (int)threadIdx.x;
+    const uint4 masked = make_uint4(Elem<T>::kMasked, Elem<T>::kMasked, Elem<T>::kMasked, Elem<T>::kMasked);
+    auto load = [&](int b, uint4 (&v)[kBatch]) {
+        const int at = sh.v0 + b * (kBatch * NT) + tid;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) v[u] = at + u * NT < sh.v1 ? ld_stream(sh.vec(at + u * NT)) : masked;
+    };
+    Running<T, false> run;
+    uint4 now[kBatch], next[kBatch];
+    const int batches = (sh.v1 - sh.v0 + kBatch * NT - 1) / (kBatch * NT);
+    if (batches > 0) load(0, now);
+    load_teacher<T, NT>(sh, p, row, &te, marks);
+    const uint8_t* mark = reinterpret_cast<const uint8_t*>(marks);
+    for (int b = 0; b < batches; ++b) {
+        if (b + 1 < batches) load(b + 1, next);
+        const int at = b * (kBatch * NT) + tid;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+            if (sh.v0 + at + u * NT < sh.v1) {
+                const uint32_t bits = mark[at + u * NT + 1];
+                if (bits) Elem<T>::mask(now[u], bits);
+            }
+        run.batch(now, p.c);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) now[u] = next[u];
+    }
+    if (sh.single >= 0) {
+        constexpr int E = Elem<T>::E;
+        const int at = sh.single - (sh.head + sh.v0 * E) + E;
+        if (!((mark[at / E] >> (at % E)) & 1)) run.one(Elem<T>::get(sh.row + sh.single), p.c);
+    }
+    Stats st;
+    run.sums(st.s, st.t);
+    st.m = run.m;
+    st.bad = run.bad ? 1 : 0;
+    st = join_row<NT>(st, warps, &mine, p.ctas, p.c);
+    if (rank == 0 && tid < 32) {
+        finish_row(p, &te, st, 0.0f);
+        __syncwarp();
+        const float loss = loss_of_row(p, &te);
+        if (tid == 0) p.loss[row] = loss;
+    }
+    __syncwarp();
+    if (p.ctas > 1) ptx::cluster_sync();
+}
+
+constexpr int kGradThreads = 512;
+
+template <typename T>
+__device__ __forceinline__ T from_float(float x);
+template <>
+__device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// Four groups of a thread's vectors are on their way into shared memory at once; the sums of a group are taken
+// while the later ones arrive.  The row stays there until its sums are known, and its gradient is written from there, so
+// logits are read once.
+template <typename T>
+__global__ void __launch_bounds__(kGradThreads)
+distill_grad_kernel(const T* logits, T* grad, int marks_at, const DistillParams p) {
+    constexpr int NT = kGradThreads, E = Elem<T>::E;
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ Stats warps[NT / 32];
+    __shared__ Stats mine;
+    __shared__ Teacher te;
+    uint32_t* marks = reinterpret_cast<uint32_t*>(smem + marks_at);
+    pdl_wait();
+    const int row = (int)blockIdx.x / p.ctas, rank = (int)blockIdx.x % p.ctas;
+    const Share<T> sh(logits + (long long)row * p.ld, p.vocab, rank, p.ctas);
+    const int tid = (int)threadIdx.x;
+    // element j of the row is kept[j - origin]: the vectors stay vectors, the elements before them end at the first
+    T* kept = reinterpret_cast<T*>(smem);
+    const int origin = sh.head + sh.v0 * E - E;
+    const uint32_t kept_addr = ptx::smem_u32(smem);
+    const int nv = sh.v1 - sh.v0;
+    const int per_thread = (nv + NT - 1) / NT, group = (per_thread + 3) / 4;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        for (int i = g * group; i < (g + 1) * group; ++i) {
+            const int v = i * NT + tid;
+            if (v < nv) ptx::cp_async_16(kept_addr + 16u * (uint32_t)(v + 1), sh.vec(sh.v0 + v));
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    if (sh.single >= 0) kept[sh.single - origin] = from_float<T>(Elem<T>::get(sh.row + sh.single));
+    const float w = p.dloss != nullptr ? ld(p.dloss + row) : 0.0f;
+    load_teacher<T, NT>(sh, p, row, &te, marks);
+    const uint8_t* mark = reinterpret_cast<const uint8_t*>(marks);
+
+    Running<T, false> run;
+    const uint4 masked = make_uint4(Elem<T>::kMasked, Elem<T>::kMasked, Elem<T>::kMasked, Elem<T>::kMasked);
+    const uint4* kept_vec = reinterpret_cast<const uint4*>(smem) + 1;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        if (g == 0) asm volatile("cp.async.wait_group 3;" ::: "memory");
+        if (g == 1) asm volatile("cp.async.wait_group 2;" ::: "memory");
+        if (g == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        if (g == 3) asm volatile("cp.async.wait_group 0;" ::: "memory");
+        for (int i = g * group; i < (g + 1) * group; i += kBatch) {
+            uint4 now[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const int v = (i + u) * NT + tid;
+                now[u] = masked;
+                if (i + u < (g + 1) * group && v < nv) {
+                    now[u] = kept_vec[v];
+                    const uint32_t bits = mark[v + 1];
+                    if (bits) Elem<T>::mask(now[u], bits);
+                }
+            }
+            run.batch(now, p.c);
+        }
+    }
+    if (sh.single >= 0) {
+        const int at = sh.single - origin;
+        if (!((mark[at / E] >> (at % E)) & 1)) run.one(Elem<T>::get(sh.row + sh.single), p.c);
+    }
+    Stats st;
+    run.sums(st.s, st.t);
+    st.m = run.m;
+    st.bad = run.bad ? 1 : 0;
+    st = join_row<NT>(st, warps, &mine, p.ctas, p.c);  // (its barriers also make the whole share visible to all threads)
+    if (tid < 32) finish_row(p, &te, st, w);
+    __syncthreads();
+    // a row that counts nothing has no gradient, whatever its logits hold; one without a distribution has NaN
+    const bool zero = w == 0.0f, none = !zero && te.none;
+    const float f = zero ? 0.0f : none ? quiet_nan() : te.scale_rest, f_own = none ? quiet_nan() : te.scale_own;
+    const float m_rest = te.m_rest;
+    auto value = [&](float x) {  // (of the teacher's tokens, whose exponent may overflow, it is overwritten)
+        const float e = ex2((x - m_rest) * p.c) * f;
+        return zero ? 0.0f : e;
+    };
+    T* out = grad + (long long)row * p.ldd;
+    // whole vectors of the result, whose rows need not start like those of the logits
+    const int before = min(sh.last - sh.first, (int)(((16u - (uint32_t)(reinterpret_cast<uintptr_t>(out + sh.first) & 15u)) & 15u) / sizeof(T)));
+    const int nout = (sh.last - sh.first - before) / E;
+    const int start = sh.first + before;  // the element they begin with
+    uint4* out_vec = reinterpret_cast<uint4*>(out + start);
+    const int pos = start - origin;       // and its place in shared memory
+    if (pos % E == 0) {
+        for (int v = tid; v < nout; v += NT) {
+            const uint4 x = reinterpret_cast<const uint4*>(smem)[pos / E + v];
+            uint32_t y[4];
+            if constexpr (E == 4) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = __float_as_uint(value(Elem<T>::at(x, i)));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(value(Elem<T>::at(x, 2 * i)), value(Elem<T>::at(x, 2 * i + 1)));
+                    memcpy(&y[i], &h, 4);
+                }
+            }
+            out_vec[v] = make_uint4(y[0], y[1], y[2], y[3]);
+        }
+    } else {
+        for (int v = tid; v < nout; v += NT) {
+            uint32_t y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const T* from = kept + pos + v * E + i * (E / 4);
+                if constexpr (E == 4) {
+                    y[i] = __float_as_uint(value(from[0]));
+                } else {
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(value(__bfloat162float(from[0])), value(__bfloat162float(from[1])));
+                    memcpy(&y[i], &h, 4);
+                }
+            }
+            out_vec[v] = make_uint4(y[0], y[1], y[2], y[3]);
+        }
+    }
+    // single elements at both ends
+    const int after = start + nout * E;
+    int at = -1;
+    if (tid < before) at = sh.first + tid;
+    if (tid >= E && tid < E + (sh.last - after)) at = after + tid - E;
+    if (at >= 0) out[at] = from_float<T>(value((float)kept[at - origin]));
+    __syncthreads();
+    // the teacher's tokens, over what the loops above wrote for them
+    if (tid < p.k && te.first[tid] && te.index[tid] >= sh.first && te.index[tid] < sh.last) {
+        double sum = te.p[tid];
+        if (te.repeated)
+            for (int i = tid + 1; i < p.k; ++i)
+                if (te.index[i] == te.index[tid]) sum += te.p[i];
+        const float q = ex2((te.x[tid] - te.m) * p.c) * f_own;
+        out[te.index[tid]] = from_float<T>(zero ? 0.0f : q - (float)(sum * masses(p, &te).keep) * (w * p.inv_t));
+    }
+    // the loss, while the other warps are done or still write
+    if (rank == 0 && p.loss != nullptr && tid >= NT - 32) {
+        const float loss = loss_of_row(p, &te);
+        if (tid == NT - 32) p.loss[row] = loss;
+    }
+    __syncwarp();
+    if (p.ctas > 1) ptx::cluster_sync();
+}
+
+// ---------------------------------------------------------------- host side
+
+bcq_status check_rows(int n, int vocab, const void* logits, size_t ld, int dtype, float temperature) {
+    if (n < 0 || vocab < 1 || ld < (size_t)vocab) return BCQ_ERR_SHAPE;
+    if (vocab > kVocabMax) return BCQ_ERR_UNSUPPORTED;
+    if (dtype != BCQ_F32 && dtype != BCQ_BF16) return BCQ_ERR_UNSUPPORTED;
+    if (!(temperature >= 1e-3f && temperature <= 1e3f)) return BCQ_ERR_SHAPE;
+    if (n > 0 && logits == nullptr) return BCQ_ERR_NULL;
+    if ((reinterpret_cast<uintptr_t>(logits) & (dtype == BCQ_BF16 ? 1u : 3u)) != 0) return BCQ_ERR_ALIGN;
+    return BCQ_OK;
+}
+
+float exponent_scale(float temperature) { return (float)(1.4426950408889634074 / (double)temperature); }
+
+// CTAs of a row: as many as leave every SM no more than `per_sm` CTAs, and every CTA a batch or so.
+int ctas_for(int n, int vocab, int elem_bytes, int threads, int per_sm) {
+    const long long nvec = (long long)vocab * elem_bytes / 16;
+    int ctas = 1;
+    while (ctas < 8 && (long long)n * ctas * 2 <= (long long)sm_count() * per_sm && nvec / (ctas * 2) >= threads) ctas *= 2;
+    return ctas;
+}
+
+int max_vectors(int vocab, int elem_bytes, int ctas) { return ceil_div(vocab * elem_bytes / 16, ctas); }
+
+template <typename T>
+bcq_status launch_logprobs(int n, const void* logits, LogprobParams p, cudaStream_t s) {
+    const int nv = max_vectors(p.vocab, (int)sizeof(T), p.ctas);
+    const size_t smem = p.top > 0 ? sizeof(TopShared) + (size_t)ceil_div(nv, kBatch * kLpThreads) * kLpThreads * 4 : 0;
+    const dim3 grid((unsigned)(n * p.ctas));
+    if (p.top > 0) {
+        const bcq_status st = ensure_dynamic_smem(token_logprobs_kernel<T, true>, smem);
+        if (st != BCQ_OK) return st;
+        BCQ_CUDA_TRY(launch_pdl(token_logprobs_kernel<T, true>, grid, kLpThreads, smem, s, (unsigned)p.ctas, (const T*)logits, p));
+    } else {
+        BCQ_CUDA_TRY(launch_pdl(token_logprobs_kernel<T, false>, grid, kLpThreads, 0, s, (unsigned)p.ctas, (const T*)logits, p));
+    }
+    return BCQ_OK;
+}
+
+template <typename T>
+bcq_status launch_loss(int n, const void* logits, const DistillParams& p, cudaStream_t s) {
+    const size_t smem = align_up((size_t)max_vectors(p.vocab, (int)sizeof(T), p.ctas) + 2, 16);
+    const bcq_status st = ensure_dynamic_smem(distill_loss_kernel<T>, smem);
+    if (st != BCQ_OK) return st;
+    BCQ_CUDA_TRY(launch_pdl(distill_loss_kernel<T>, dim3((unsigned)(n * p.ctas)), kLossThreads, smem, s, (unsigned)p.ctas,
+                            (const T*)logits, p));
+    return BCQ_OK;
+}
+
+// Shared memory of a CTA of the gradient: its vectors, one more before and after, the marks.
+size_t grad_kept_bytes(int vocab, int elem_bytes, int ctas) { return (size_t)(max_vectors(vocab, elem_bytes, ctas) + 2) * 16; }
+size_t grad_smem_bytes(int vocab, int elem_bytes, int ctas) {
+    return grad_kept_bytes(vocab, elem_bytes, ctas) + align_up((size_t)max_vectors(vocab, elem_bytes, ctas) + 2, 16);
+}
+
+template <typename T>
+bcq_status launch_grad(int n, const void* logits, void* grad, DistillParams p, cudaStream_t s) {
+    p.ctas = ctas_for(n, p.vocab, (int)sizeof(T), kGradThreads, 2);
+    // two CTAs of an SM, so that one reads while the other writes
+    while (p.ctas < 8 && grad_smem_bytes(p.vocab, (int)sizeof(T), p.ctas) > 108 * 1024) p.ctas *= 2;
+    const size_t smem = grad_smem_bytes(p.vocab, (int)sizeof(T), p.ctas);
+    const bcq_status st = ensure_dynamic_smem(distill_grad_kernel<T>, smem);
+    if (st != BCQ_OK) return st;
+    BCQ_CUDA_TRY(launch_pdl(distill_grad_kernel<T>, dim3((unsigned)(n * p.ctas)), kGradThreads, smem, s, (unsigned)p.ctas,
+                            (const T*)logits, (T*)grad, (int)grad_kept_bytes(p.vocab, (int)sizeof(T), p.ctas), p));
+    return BCQ_OK;
+}
+
+bcq_status check_teacher(int n, int k, const int* index, const float* logp) {
+    if (k < 1) return BCQ_ERR_SHAPE;
+    if (k > kTopMax) return BCQ_ERR_UNSUPPORTED;
+    if (n > 0 && (!index || !logp)) return BCQ_ERR_NULL;
+    return BCQ_OK;
+}
+
+}  // namespace
+
+extern "C" bcq_status bcq_token_logprobs(int n, int vocab, const void* logits, size_t ld, int dtype, const long long* targets,
+                                         int top_k, float temperature, float* logprob, float* entropy, float* top_logprob,
+                                         int* top_index, void* stream) {
+    const bcq_status st = check_rows(n, vocab, logits, ld, dtype, temperature);
+    if (st != BCQ_OK) return st;
+    if (top_k < 0) return BCQ_ERR_SHAPE;
+    if (top_k > kTopMax) return BCQ_ERR_UNSUPPORTED;
+    if (n == 0) return BCQ_OK;
+    if ((targets == nullptr) != (logprob == nullptr)) return BCQ_ERR_NULL;
+    if (top_k > 0 && (!top_logprob || !top_index)) return BCQ_ERR_NULL;
+    LogprobParams p;
+    p.vocab = vocab; p.top = top_k;
+    p.ld = (long long)ld;
+    p.targets = targets;
+    p.c = exponent_scale(temperature); p.inv_t = 1.0f / temperature;
+    p.logprob = logprob; p.entropy = entropy; p.top_logprob = top_logprob; p.top_index = top_index;
+    p.ctas = ctas_for(n, vocab, dtype == BCQ_BF16 ? 2 : 4, kLpThreads, 3);
+    cudaStream_t s = (cudaStream_t)stream;
+    return dtype == BCQ_BF16 ? launch_logprobs<__nv_bfloat16>(n, logits, p, s) : launch_logprobs<float>(n, logits, p, s);
+}
+
+extern "C" bcq_status bcq_distill_loss(int n, int vocab, int k, const void* logits, size_t ld, int dtype, const int* top_index,
+                                       const float* top_logprob, float temperature, int tail, float* loss, void* stream) {
+    bcq_status st = check_rows(n, vocab, logits, ld, dtype, temperature);
+    if (st != BCQ_OK) return st;
+    if ((st = check_teacher(n, k, top_index, top_logprob)) != BCQ_OK) return st;
+    if (n == 0) return BCQ_OK;
+    if (!loss) return BCQ_ERR_NULL;
+    DistillParams p;
+    p.vocab = vocab; p.k = k; p.tail = tail != 0; p.ld = (long long)ld; p.ldd = 0;
+    p.index = top_index; p.logp = top_logprob; p.dloss = nullptr;
+    p.c = exponent_scale(temperature); p.inv_t = 1.0f / temperature; p.inv_t64 = 1.0 / (double)temperature;
+    p.loss = loss;
+    p.ctas = ctas_for(n, vocab, dtype == BCQ_BF16 ? 2 : 4, kLossThreads, 3);
+    cudaStream_t s = (cudaStream_t)stream;
+    return dtype == BCQ_BF16 ? launch_loss<__nv_bfloat16>(n, logits, p, s) : launch_loss<float>(n, logits, p, s);
+}
+
+extern "C" bcq_status bcq_distill_grad(int n, int vocab, int k, const void* logits, size_t ld, int dtype, const int* top_index,
+                                       const float* top_logprob, float temperature, int tail, const float* dloss, float* loss,
+                                       void* dlogits, size_t lddl, void* stream) {
+    bcq_status st = check_rows(n, vocab, logits, ld, dtype, temperature);
+    if (st != BCQ_OK) return st;
+    if ((st = check_teacher(n, k, top_index, top_logprob)) != BCQ_OK) return st;
+    if (lddl < (size_t)vocab) return BCQ_ERR_SHAPE;
+    if (n == 0) return BCQ_OK;
+    if (!dloss || !dlogits) return BCQ_ERR_NULL;
+    if ((reinterpret_cast<uintptr_t>(dlogits) & (dtype == BCQ_BF16 ? 1u : 3u)) != 0) return BCQ_ERR_ALIGN;
+    if (dlogits == logits && lddl != ld) return BCQ_ERR_SHAPE;
+    DistillParams p;
+    p.vocab = vocab; p.k = k; p.tail = tail != 0; p.ld = (long long)ld; p.ldd = (long long)lddl;
+    p.index = top_index; p.logp = top_logprob; p.dloss = dloss;
+    p.c = exponent_scale(temperature); p.inv_t = 1.0f / temperature; p.inv_t64 = 1.0 / (double)temperature;
+    p.loss = loss; p.ctas = 1;
+    cudaStream_t s = (cudaStream_t)stream;
+    return dtype == BCQ_BF16 ? launch_grad<__nv_bfloat16>(n, logits, dlogits, p, s) : launch_grad<float>(n, logits, dlogits, p, s);
+}
