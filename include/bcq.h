@@ -262,6 +262,34 @@ bcq_status bcq_alpha_pack(long long count, int nseg, const long long* seg_begin,
 bcq_status bcq_alpha_unpack(long long count, int nseg, const long long* seg_begin, const long long* seg_prefix,
                             const float* packed, float* alpha_flat, void* stream);
 
+/* ------------------------------------------------------------------ microscaled 4-bit floating point
+ *
+ * The other 4-bit form of a matrix: what the tensor core multiplies as it is (the OCP microscaling format MXFP4).  Blocks of 32
+ * consecutive elements of a row share a power of two, the last block of a row may be shorter; an element is a sign and one of
+ * 0, 1/2, 1, 3/2, 2, 3, 4, 6 times it.  A matrix of `rows` x `cols` (cols <= 2^20) is held in two buffers, both 16-byte aligned:
+ *   codes  : uint8 [rows][64 * ceil(cols / 128)], element k of a row in byte k / 2, even k in the low half; bit 3 is the sign, bits
+ *            0 - 2 number the magnitudes above.  Elements behind a row's last are 0.
+ *   scales : uint8 [ceil(rows / 128)][ceil(cols / 128)][32][4][4], exponent + 127 of row r and block b at
+ *            [r / 128][b / 4][r % 32][(r / 32) % 4][b % 4]; 255 is NaN.  Rows and blocks behind the last are 0. */
+
+/* Bytes of the two buffers.  0 if a size is < 1. */
+size_t bcq_mx_codes_bytes(int rows, int cols);
+size_t bcq_mx_scales_bytes(int rows, int cols);
+
+/* X [rows][ldx] (BCQ_F32 or BCQ_BF16, any alignment; rows that are 16-byte aligned are read faster) to codes and scales: a block's
+ * exponent is floor(log2 max|x|) - 2, at least -127; x 2^-e goes to the nearest magnitude, ties to the even code, larger ones to 6.
+ * A block that holds a NaN or an infinity gets the scale NaN.  rows = 0 is allowed. */
+bcq_status bcq_mx_quantize(int rows, int cols, const void* X, size_t ldx, int x_dtype, uint8_t* codes, uint8_t* scales, void* stream);
+/* The values that codes and scales stand for, exactly (in bf16 too). */
+bcq_status bcq_mx_dequantize(int rows, int cols, const uint8_t* codes, const uint8_t* scales, void* X_hat, size_t ldx, int x_dtype,
+                             void* stream);
+
+/* Y[t][j] = sum_k X_hat[t][k] W_hat[j][k] (+ bias[j]): n tokens (x_codes, x_scales of n x d_in) through a matrix (w_codes, w_scales of
+ * d_out x d_in), for one token as for thousands.  Products are exact and accumulated in fp32 by the tensor core, in a fixed order for
+ * given sizes.  bias: float [d_out] or NULL; Y: y_dtype [n][ldy], ldy >= d_out.  No workspace; n = 0 is allowed. */
+bcq_status bcq_mx_linear(int d_out, int d_in, int n, const uint8_t* x_codes, const uint8_t* x_scales, const uint8_t* w_codes,
+                         const uint8_t* w_scales, const float* bias, void* Y, size_t ldy, int y_dtype, void* stream);
+
 /* ------------------------------------------------------------------ logits: answers and losses
  *
  * Operators over n rows of `vocab` logits, dtype BCQ_F32 or BCQ_BF16, row pitch ld >= vocab elements.  Rows may start at

@@ -28,7 +28,8 @@ SYMBOLS = ("bcq_pitch_words", "bcq_bits_bytes", "bcq_num_groups", "bcq_alpha_cou
            "bcq_decode_pack", "bcq_linear_decode_packed", "bcq_lr_linear_decay", "bcq_alpha_adamw",
            "bcq_alpha_pack", "bcq_alpha_unpack", "bcq_prepared_bytes", "bcq_prepare_planes",
            "bcq_linear_fwd_prepared", "bcq_linear_bwd_x_prepared", "bcq_check_device", "bcq_token_logprobs",
-           "bcq_distill_loss", "bcq_distill_grad")
+           "bcq_distill_loss", "bcq_distill_grad", "bcq_mx_codes_bytes", "bcq_mx_scales_bytes", "bcq_mx_quantize",
+           "bcq_mx_dequantize", "bcq_mx_linear")
 
 
 class BcqError(RuntimeError):
@@ -105,6 +106,16 @@ def lib() -> C.CDLL:
         l.bcq_distill_loss.argtypes = [i, i, i, vp, sz, i, vp, vp, f32, i, vp, vp]
         l.bcq_distill_grad.restype = i
         l.bcq_distill_grad.argtypes = [i, i, i, vp, sz, i, vp, vp, f32, i, vp, vp, vp, sz, vp]
+        l.bcq_mx_codes_bytes.restype = sz
+        l.bcq_mx_codes_bytes.argtypes = [i, i]
+        l.bcq_mx_scales_bytes.restype = sz
+        l.bcq_mx_scales_bytes.argtypes = [i, i]
+        l.bcq_mx_quantize.restype = i
+        l.bcq_mx_quantize.argtypes = [i, i, vp, sz, i, vp, vp, vp]
+        l.bcq_mx_dequantize.restype = i
+        l.bcq_mx_dequantize.argtypes = [i, i, vp, vp, vp, sz, i, vp]
+        l.bcq_mx_linear.restype = i
+        l.bcq_mx_linear.argtypes = [i, i, i, vp, vp, vp, vp, vp, vp, sz, i, vp]
         l.bcq_status_string.restype = C.c_char_p
         l.bcq_status_string.argtypes = [i]
         l.bcq_last_cuda_error.restype = i
@@ -450,7 +461,7 @@ def alpha_unpack(packed, alpha_flat, segments: Segments):
                                   _ptr(packed), _ptr(alpha_flat), _stream()), "bcq_alpha_unpack")
 
 
-# ---------------------------------------------------------------------------- logits: answers and losses
+# ---------------------------------------------------------------------------- operands of the calls below
 
 def _device_of(name, t, dtype=None, shape=None):
     """Checks an operand: on the current device (the stream is that device's), of the type and shape given, dense."""
@@ -470,6 +481,70 @@ def _rows(name, t):
     n, cols = t.shape
     return n, cols, t.stride(0) if n > 1 else max(cols, t.stride(0))
 
+
+# ---------------------------------------------------------------------------- microscaled 4-bit floating point
+
+class MxMatrix:
+    """A matrix in microscaled 4-bit floating point: codes uint8 [rows][64 * ceil(cols / 128)] and scales uint8
+    [ceil(rows / 128)][ceil(cols / 128)][32][4][4] (the container of include/bcq.h)."""
+
+    def __init__(self, codes, scales, rows: int, cols: int):
+        torch = _torch()
+        if rows < 0 or cols < 1:
+            raise ValueError("rows must be at least 0, cols at least 1")
+        a = -(-cols // 128)
+        _device_of("codes", codes, torch.uint8, (rows, 64 * a))
+        _device_of("scales", scales, torch.uint8, (-(-rows // 128), a, 32, 4, 4))
+        self.codes, self.scales, self.rows, self.cols = codes, scales, rows, cols
+
+
+def mx_quantize(X) -> MxMatrix:
+    """bcq_mx_quantize: X fp32 or bf16 [rows][cols] to microscaled 4-bit floating point."""
+    torch = _torch()
+    _device_of("X", X)
+    rows, cols, ld = _rows("X", X)
+    a = -(-cols // 128)
+    codes = _empty(X, (rows, 64 * a), torch.uint8)
+    scales = _empty(X, (-(-rows // 128), a, 32, 4, 4), torch.uint8)
+    _check(_fn().mx_quantize(rows, cols, _ptr(X), ld, _dtype_code(X), _ptr(codes), _ptr(scales), _stream()), "bcq_mx_quantize")
+    return MxMatrix(codes, scales, rows, cols)
+
+
+def mx_dequantize(M: MxMatrix, out_dtype=None):
+    """bcq_mx_dequantize: the values of M, fp32 or (as exactly) bf16."""
+    torch = _torch()
+    _device_of("M", M.codes)
+    out = _empty(M.codes, (M.rows, M.cols), out_dtype or torch.float32)
+    _check(_fn().mx_dequantize(M.rows, M.cols, _ptr(M.codes), _ptr(M.scales), _ptr(out), M.cols, _dtype_code(out), _stream()),
+           "bcq_mx_dequantize")
+    return out
+
+
+def mx_linear(X, W: MxMatrix, bias=None, out=None, out_dtype=None):
+    """bcq_mx_linear: X (an MxMatrix [n][d_in], or fp32 or bf16 values that are quantised first) through W [d_out][d_in] -> Y
+    [n][d_out], fp32 unless ``out`` or ``out_dtype`` says bf16.  The same call serves one token and a whole prompt."""
+    torch = _torch()
+    if not isinstance(X, MxMatrix):
+        X = mx_quantize(X)
+    if X.cols != W.cols:
+        raise ValueError("X has %d columns, W %d" % (X.cols, W.cols))
+    _device_of("X", X.codes)
+    _device_of("W", W.codes)
+    n, d_out = X.rows, W.rows
+    if bias is not None:
+        _device_of("bias", bias, torch.float32, (d_out,))
+    if out is None:
+        out = _empty(X.codes, (n, d_out), out_dtype or torch.float32)
+    _device_of("out", out, out_dtype)
+    if tuple(out.shape) != (n, d_out):
+        raise ValueError("out must have shape %s" % [n, d_out])
+    _, _, ldy = _rows("out", out)
+    _check(_fn().mx_linear(d_out, W.cols, n, _ptr(X.codes), _ptr(X.scales), _ptr(W.codes), _ptr(W.scales), _ptr(bias), _ptr(out), ldy,
+                           _dtype_code(out), _stream()), "bcq_mx_linear")
+    return out
+
+
+# ---------------------------------------------------------------------------- logits: answers and losses
 
 def token_logprobs(logits, targets=None, top_k: int = 0, temperature: float = 1.0):
     """bcq_token_logprobs: logits bf16 or fp32 [n][vocab], targets int64 [n] or None -> (logprob fp32 [n] or None, entropy

@@ -144,6 +144,7 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 // per-TU device timeout flags
 bcq_status expand_timeout_flag(int* flag_out, int reset);
 bcq_status dalpha_timeout_flag(int* flag_out, int reset);
+bcq_status mx_timeout_flag(int* flag_out, int reset);
 
 // decode from the canonical planes (decode.cu); the arguments have been checked
 bcq_status run_decode_planes(int d_out, int d_in, int q, int g, int n, const void* X, size_t ldx, const uint32_t* bits,

@@ -1,0 +1,631 @@
+// Microscaled 4-bit floating point: quantisation, its inverse, and the product of two matrices that are stored so.
+//
+// Blocks of 32 consecutive elements of a row share a power of two, 2^e with e = floor(log2 max|x|) - 2 (at least -127), and an element
+// is x 2^-e rounded to the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 (ties to the even code, larger ones to 6).
+//
+// The product runs on the tensor core's own block-scaled instruction (kind::mxf4): the codes go from memory to it as they
+// are, the scales by way of tensor memory, and products are accumulated in fp32.  Weights are the operand of 128 rows (M),
+// tokens the other (N = 16 .. 256): so one token costs a narrow instruction, not a wide one with empty rows, and a
+// warp's 32 accumulator lanes are 32 consecutive outputs of a token, which it writes as they are.
+#include <algorithm>
+
+#include "gemm_common.cuh"
+
+namespace {
+
+using namespace bcq;
+
+__device__ int g_timeout_flag = 0;
+
+constexpr int kMxMaxCols = 1 << 20;
+
+inline size_t mx_pitch(int cols) { return (size_t)64 * (((size_t)cols + 127) / 128); }
+inline int mx_atoms(int cols) { return ceil_div(cols, 128); }
+
+// ---------------------------------------------------------------- quantisation
+
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// Eight values to eight codes, the first in the lowest bits.
+__device__ __forceinline__ uint32_t to_e2m1_x8(const float (&v)[8]) {
+    uint32_t r;
+    asm("{\n\t"
+        ".reg .b8 b0, b1, b2, b3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
+        "mov.b32 %0, {b0, b1, b2, b3};\n\t"
+        "}\n"
+        : "=r"(r)
+        : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return r;
+}
+
+__device__ __forceinline__ float load_one(const float* p) { return ld(p); }
+__device__ __forceinline__ float load_one(const __nv_bfloat16* p) {
+    unsigned short h;
+    asm volatile("ld.global.u16 %0, [%1];" : "=h"(h) : "l"(p));
+    return __uint_as_float((uint32_t)h << 16);
+}
+__device__ __forceinline__ void load_eight(const float* p, float (&v)[8]) {
+    const float4 a = ld_stream(reinterpret_cast<const float4*>(p)), b = ld_stream(reinterpret_cast<const float4*>(p) + 1);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void load_eight(const __nv_bfloat16* p, float (&v)[8]) {
+    const uint4 a = ld_stream(reinterpret_cast<const uint4*>(p));
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+
+// Where the four scales of 128 elements of a row are, as one word.
+__device__ __forceinline__ long long scale_word(long long row, int atom, int atoms) {
+    return (((row >> 7) * atoms + atom) * 32 + (row & 31)) * 4 + ((row >> 5) & 3);
+}
+
+struct MxQuantParams {
+    int rows, cols, atoms, vec;  // vec: rows are 16-byte aligned
+    long long ld, pitch, units;  // units: (row of the padded 128s, atom)
+};
+
+// Sixteen lanes have 128 elements of a row, eight each: four of them a block.  Bound by memory.  A lane has
+// kUnits such pieces on their way at once.
+constexpr int kUnits = 4;
+
+template <typename T>
+__global__ void __launch_bounds__(256)
+mx_quantize_kernel(const T* X, uint8_t* codes, uint32_t* scales, const MxQuantParams p) {
+    pdl_trigger();
+    pdl_wait();
+    const int lane16 = (int)threadIdx.x & 15;
+    const long long group = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 4;
+    const long long groups = ((long long)gridDim.x * blockDim.x) >> 4;
+    // (units are an even number, as rows come in 128s: both groups of a warp take every turn, as the shuffles want)
+    for (long long first = group; first < p.units; first += groups * kUnits) {
+        float v[kUnits][8];
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const long long unit = first + u * groups;
+            const long long row = unit / p.atoms;
+            const int col = (int)(unit - row * p.atoms) * 128 + lane16 * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[u][i] = 0.0f;
+            if (unit < p.units && row < p.rows) {
+                const T* src = X + row * p.ld + col;
+                if (p.vec && col + 8 <= p.cols) {
+                    load_eight(src, v[u]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (col + i < p.cols) v[u][i] = load_one(src + i);
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const long long unit = first + u * groups;
+            uint32_t top = 0;  // (as whole numbers: NaN and infinity are the largest)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = max(top, abs_bits(v[u][i]));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const bool finite = top < 0x7f800000u;
+            // the exponent field is floor(log2) + 127 (0 for what is below 2^-126, whose scale is the smallest too)
+            const uint32_t s = finite ? (uint32_t)max(0, (int)(top >> 23) - 2) : 255u;
+            const float f = __uint_as_float((254u - (finite ? s : 0u)) << 23);  // 2^(127 - s)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[u][i] = finite ? v[u][i] * f : 0.0f;
+            const uint32_t c = to_e2m1_x8(v[u]);
+            // the four blocks' scales to the first lane
+            uint32_t word = s << (8 * ((lane16 >> 2) & 3));
+            word |= __shfl_xor_sync(0xffffffffu, word, 4);
+            word |= __shfl_xor_sync(0xffffffffu, word, 8);
+            if (unit < p.units) {
+                const long long row = unit / p.atoms;
+                const int atom = (int)(unit - row * p.atoms);
+                if (row < p.rows) *reinterpret_cast<uint32_t*>(codes + row * p.pitch + atom * 64 + lane16 * 4) = c;
+                if (lane16 == 0) scales[scale_word(row, atom, p.atoms)] = word;
+            }
+        }
+    }
+}
+
+// 2^(s - 127); 255 is NaN.
+__device__ __forceinline__ float scale_value(uint32_t s) {
+    return __uint_as_float(s == 0 ? 0x00400000u : s == 255u ? 0x7fc00000u : s << 23);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256)
+mx_dequantize_kernel(const uint8_t* codes, const uint32_t* scales, T* X, const MxQuantParams p) {
+    pdl_wait();
+    const int lane16 = (int)threadIdx.x & 15;
+    const long long group = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 4;
+    const long long groups = ((long long)gridDim.x * blockDim.x) >> 4;
+    for (long long first = group; first < p.units; first += groups * kUnits) {
+        uint32_t c[kUnits], s[kUnits];
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const long long unit = first + u * groups;
+            c[u] = s[u] = 0;
+            if (unit < p.units) {
+                const long long row = unit / p.atoms;
+                const int atom = (int)(unit - row * p.atoms);
+                c[u] = ld_stream(reinterpret_cast<const uint32_t*>(codes + row * p.pitch + atom * 64 + lane16 * 4));
+                s[u] = ld(scales + scale_word(row, atom, p.atoms));
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const long long unit = first + u * groups;
+            if (unit >= p.units) break;
+            const long long row = unit / p.atoms;
+            const int col = (int)(unit - row * p.atoms) * 128 + lane16 * 8;
+            const float f = scale_value((s[u] >> (8 * (lane16 >> 2))) & 255u);
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t code = (c[u] >> (4 * i)) & 15u;
+                // exponent and mantissa bits of the code in those of a float: the value times 2^-126 (subnormal codes included)
+                const float a = __uint_as_float(((code & 7u) << 22) | ((code & 8u) << 28)) * __uint_as_float(253u << 23);
+                v[i] = a * f;
+            }
+            T* dst = X + row * p.ld + col;
+            if (p.vec && col + 8 <= p.cols) {
+                if constexpr (sizeof(T) == 4) {
+                    reinterpret_cast<float4*>(dst)[0] = make_float4(v[0], v[1], v[2], v[3]);
+                    reinterpret_cast<float4*>(dst)[1] = make_float4(v[4], v[5], v[6], v[7]);
+                } else {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+                        memcpy(&w[i], &h, 4);
+                    }
+                    *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (col + i < p.cols) {
+                        if constexpr (sizeof(T) == 4) dst[i] = v[i];
+                        else dst[i] = __float2bfloat16_rn(v[i]);
+                    }
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- product
+
+struct MxLinearParams {
+    int d_out, n;
+    int atoms;           // ceil(d_in / 128)
+    int m_tiles, n_tiles;
+    int steps;           // of 256 elements of d_in: ceil(atoms / 2)
+    int splits;          // CTAs of a cluster, which share a tile's steps
+    const uint8_t* w_scales;
+    const uint8_t* x_scales;
+    const float* bias;
+    void* Y;
+    long long ldy;
+};
+
+// BN tokens by 128 outputs.  A stage holds 256 elements of d_in: 128 bytes of codes a row, two atoms of scales a 128 rows.
+template <int BN>
+struct MxTile {
+    static constexpr int kRowBlocks = (BN + 127) / 128;             // of the tokens' scales
+    static constexpr uint32_t kA = 128 * 128, kB = BN * 128;
+    static constexpr uint32_t kScaleA = 1024, kScaleB = 1024 * kRowBlocks;
+    static constexpr uint32_t kStage = kA + kB + kScaleA + kScaleB;
+    static constexpr int kPerSm = BN <= 64 ? 2 : 1;                 // CTAs
+    static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 6 : BN == 16 ? 5 : 4;
+    static constexpr int kAccs = BN == 256 ? 1 : 2;                 // accumulators: with one, a tile's is taken to registers at once
+    static constexpr uint32_t kScaleCol = kAccs * BN;               // columns of the scales: 8 + 8 per row block for each stage
+    static constexpr uint32_t kScaleCols = 8 + 8 * kRowBlocks;
+    static constexpr uint32_t kUsed = kScaleCol + kStages * kScaleCols;
+    static constexpr uint32_t kTmemCols = kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
+    static constexpr size_t kSmem = (size_t)kStages * kStage + 1024 + 256;
+    static_assert(kUsed <= 512 && kTmemCols * kPerSm <= 512, "tensor memory");
+    static_assert(kSmem <= 232448, "shared memory");
+    static_assert((size_t)kStages * kStage >= (size_t)BN * 128 * 4, "a tile of partial sums fits over the stages");
+};
+
+template <typename Out>
+__device__ __forceinline__ void store_out(Out* p, float v) {
+    if constexpr (sizeof(Out) == 4) *p = v;
+    else *p = __float2bfloat16_rn(v);
+}
+
+// Warp 0: TMA; warp 1: scales to tensor memory and UMMA; warps 2..9: epilogue.
+template <int BN, typename Out>
+__global__ void __launch_bounds__(kThreads, MxTile<BN>::kPerSm)
+mx_linear_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const MxLinearParams p) {
+    using Tile = MxTile<BN>;
+    constexpr int S = Tile::kStages;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* smem_gen = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
+    const uint32_t ctl_base = smem_base + S * Tile::kStage;
+    uint8_t* ctl_gen = smem_gen + S * Tile::kStage;
+    // all code tiles first (1024-byte aligned), the scales behind them
+    const uint32_t scales_base = smem_base + S * (Tile::kA + Tile::kB);
+
+    Ctl ctl;
+    ctl.full = ctl_base;
+    ctl.aready = 0;
+    ctl.empty = ctl_base + 8 * S;
+    ctl.accum = ctl_base + 16 * S;              // + 8c : accumulator c complete
+    const uint32_t acc_empty = ctl.accum + 16;  // + 8c : accumulator c drained
+    ctl.spare = ctl.accum + 32;
+    volatile uint32_t* tmem_holder = reinterpret_cast<volatile uint32_t*>(ctl_gen + 16 * S + 40);
+    ctl.abort_flag = reinterpret_cast<volatile int*>(ctl_gen + 16 * S + 44);
+    ctl.device_flag = &g_timeout_flag;
+
+    const int warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
+    const int num_tiles = p.m_tiles * p.n_tiles;
+    const int rank = p.splits > 1 ? (int)ptx::cluster_rank() : 0;
+    const int tile0 = (int)blockIdx.x / p.splits, tile_step = (int)gridDim.x / p.splits;
+    const int per = (p.steps + p.splits - 1) / p.splits;
+    const int step0 = min(p.steps, rank * per), steps = min(p.steps, step0 + per) - step0;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S; ++s) {
+            ptx::mbar_init(ctl.full + 8 * s, 1);
+            ptx::mbar_init(ctl.empty + 8 * s, 1);
+        }
+        for (int c = 0; c < 2; ++c) {
+            ptx::mbar_init(ctl.accum + 8 * c, 1);
+            ptx::mbar_init(acc_empty + 8 * c, kWorkerWarps);
+        }
+        ptx::mbar_init(ctl.spare, 1);
+        *ctl.abort_flag = 0;
+        ptx::fence_mbar_init();
+        ptx::prefetch_tmap(&tmap_w);
+        ptx::prefetch_tmap(&tmap_x);
+    }
+    __syncwarp();
+    if (warp == 1) {
+        ptx::tmem_alloc(ptx::smem_u32(const_cast<uint32_t*>(tmem_holder)), Tile::kTmemCols);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    pdl_wait();
+    const uint32_t tmem_base = *tmem_holder;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            bool ok = true;
+            int s = 0;
+            uint32_t ph = 0;
+            for (int tile = tile0; tile < num_tiles && ok; tile += tile_step) {
+                const int m0 = tile % p.m_tiles, n0 = tile / p.m_tiles;
+                const int row_blocks = min(Tile::kRowBlocks, (p.n + 127) / 128 - n0 * BN / 128);
+                for (int it = 0; it < steps; ++it) {
+                    ok = wait_bar(ctl.empty + 8 * s, ph ^ 1u, ctl, 41);
+                    if (!ok) break;
+                    const int step = step0 + it;
+                    const uint32_t sa = smem_base + s * (Tile::kA + Tile::kB), sf = scales_base + s * (Tile::kScaleA + Tile::kScaleB);
+                    const uint32_t bar = ctl.full + 8 * s;
+                    const uint32_t atom_bytes = 512u * (uint32_t)min(2, p.atoms - 2 * step);
+                    ptx::mbar_arrive_expect_tx(bar, Tile::kA + Tile::kB + atom_bytes * (uint32_t)(1 + row_blocks));
+                    ptx::tma_load_2d(sa, &tmap_w, step * 128, m0 * 128, bar);
+                    ptx::tma_load_2d(sa + Tile::kA, &tmap_x, step * 128, n0 * BN, bar);
+                    ptx::bulk_load(sf, p.w_scales + ((long long)m0 * p.atoms + 2 * step) * 512, atom_bytes, bar);
+                    for (int b = 0; b < row_blocks; ++b)
+                        ptx::bulk_load(sf + Tile::kScaleA + 1024u * b,
+                                       p.x_scales + ((long long)(n0 * BN / 128 + b) * p.atoms + 2 * step) * 512, atom_bytes, bar);
+                    if (++s == S) { s = 0; ph ^= 1u; }
+                }
+            }
+            // giving up: copies may be in flight, which land within microseconds; wait a thousand times as long
+            if (!ok) for (int i = 0; i < 1000; ++i) __nanosleep(2000);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (ptx::elect_one()) {
+            bool ok = true;
+            int s = 0, lt = 0;
+            uint32_t ph = 0;
+            // descriptors (128-byte swizzle, K-major: groups of eight rows 1024 bytes apart); 64 elements are 32 bytes on
+            constexpr uint32_t kHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+            for (int tile = tile0; tile < num_tiles && ok; tile += tile_step, ++lt) {
+                const int acc = lt % Tile::kAccs, use = lt / Tile::kAccs;
+                ok = wait_bar(acc_empty + 8 * acc, (uint32_t)(use & 1) ^ 1u, ctl, 42, 32u);
+                if (!ok) break;
+                ptx::tc_fence_after_sync();
+                const uint32_t d_tmem = tmem_base + (uint32_t)(acc * BN);
+                for (int it = 0; it < steps; ++it) {
+                    ok = wait_bar(ctl.full + 8 * s, ph, ctl, 43, 32u);
+                    if (!ok) break;
+                    ptx::tc_fence_after_sync();
+                    const uint32_t sa = smem_base + s * (Tile::kA + Tile::kB), sf = scales_base + s * (Tile::kScaleA + Tile::kScaleB);
+                    // Each stage has its own columns for the scales: when its barrier says that the stage may be filled
+                    // again, the UMMAs that read them have completed too.
+                    const uint32_t col_a = tmem_base + Tile::kScaleCol + (uint32_t)s * Tile::kScaleCols, col_b = col_a + 8;
+                    const int atoms = min(2, p.atoms - 2 * (step0 + it));
+                    for (int a = 0; a < atoms; ++a) {
+                        ptx::tmem_copy_scales(col_a + 4 * a, sf + 512 * a);
+#pragma unroll
+                        for (int b = 0; b < Tile::kRowBlocks; ++b)
+                            ptx::tmem_copy_scales(col_b + 4 * (a * Tile::kRowBlocks + b), sf + Tile::kScaleA + 1024 * b + 512 * a);
+                    }
+                    const uint32_t a_lo = (sa >> 4) & 0x3FFFu, b_lo = ((sa + Tile::kA) >> 4) & 0x3FFFu;
+                    for (int a = 0; a < atoms; ++a) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int kk = 2 * a + h;
+                            ptx::umma_mxf4(d_tmem, a_lo + 2 * kk, kHi, b_lo + 2 * kk, kHi,
+                                           h ? ptx::make_idesc_mxf4(128, BN, 1) : ptx::make_idesc_mxf4(128, BN, 0), col_a + 4 * a,
+                                           col_b + 4 * a * Tile::kRowBlocks, (it > 0 || kk > 0) ? 1u : 0u);
+                        }
+                    }
+                    ptx::umma_commit(ctl.empty + 8 * s);
+                    if (++s == S) { s = 0; ph ^= 1u; }
+                }
+                if (ok) ptx::umma_commit(ctl.accum + 8 * acc);
+            }
+            if (!ok) {
+                ptx::umma_commit(ctl.spare);
+                wait_bar(ctl.spare, 0, ctl, 44);
+            }
+        }
+        __syncwarp();
+    } else {
+        // thread = (output row, half of the tile's tokens)
+        const int quarter = warp & 3;
+        const int half = (warp - kWorkerWarp0) >> 2;
+        constexpr int kCols = BN == 16 ? 16 : BN / 2;  // of a thread (16 tokens: the second half of the warps has nothing to do)
+        constexpr int kLd = kCols < 32 ? 16 : 32;
+        const bool works = BN != 16 || half == 0;
+        Out* Y = reinterpret_cast<Out*>(p.Y);
+        float* partial = reinterpret_cast<float*>(smem_gen);  // [BN][128], over the stages
+        bool ok = true;
+        int lt = 0;
+        for (int tile = tile0; tile < num_tiles && ok; tile += tile_step, ++lt) {
+            const int m0 = tile % p.m_tiles, n0 = tile / p.m_tiles;
+            const int acc = lt % Tile::kAccs, use = lt / Tile::kAccs;
+            const int jl = quarter * 32 + lane, j = m0 * 128 + jl;
+            const int tl = works ? half * kCols : 0, t0 = n0 * BN + tl;
+            const bool j_ok = j < p.d_out;
+            const float bias = p.bias != nullptr && j_ok ? ld(p.bias + j) : 0.0f;
+            ok = wait_bar(ctl.accum + 8 * acc, (uint32_t)use & 1u, ctl, 45, 64u);
+            if (!ok) break;
+            ptx::tc_fence_after_sync();
+            uint32_t v[kCols];
+            if (works) {
+#pragma unroll
+                for (int c = 0; c < kCols; c += kLd) {
+                    const uint32_t at = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * BN + tl + c);
+                    if constexpr (kLd == 16) ptx::tmem_ld_x16(at, v + c);
+                    else ptx::tmem_ld_x32(at, v + c);
+                }
+                ptx::tmem_ld_wait();
+            }
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(acc_empty + 8 * acc) : "memory");
+            if (!works) continue;
+            if (p.splits > 1) {
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) partial[(tl + c) * 128 + jl] = steps > 0 ? __uint_as_float(v[c]) : 0.0f;
+            } else if (j_ok) {
+                Out* y = Y + (long long)t0 * p.ldy + j;
+#pragma unroll
+                for (int c = 0; c < kCols; ++c)
+                    if (t0 + c < p.n) store_out(y + c * p.ldy, __uint_as_float(v[c]) + bias);
+            }
+        }
+    }
+
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    if (p.splits > 1) {
+        // the cluster's partial sums, in the order of its ranks; each CTA adds up its share of the tile
+        ptx::cluster_sync();
+        const int m0 = tile0 % p.m_tiles, n0 = tile0 / p.m_tiles;
+        const int vecs = min(BN, p.n - n0 * BN) * 32;  // of four outputs
+        const int share = (vecs + p.splits - 1) / p.splits;
+        const int last = min(vecs, (rank + 1) * share);
+        const uint32_t mine = smem_base;
+        Out* Y = reinterpret_cast<Out*>(p.Y);
+        for (int e = rank * share + (int)threadIdx.x; e < last; e += kThreads) {
+            float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int r = 0; r < p.splits; ++r) {
+                const float4 f = ptx::ld_cluster_v4(ptx::cluster_addr(mine + 16u * (uint32_t)e, (uint32_t)r));
+                sum.x += f.x; sum.y += f.y; sum.z += f.z; sum.w += f.w;
+            }
+            const int t = n0 * BN + e / 32, j = m0 * 128 + (e & 31) * 4;
+            const float s4[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (j + i < p.d_out) store_out(Y + (long long)t * p.ldy + j + i, s4[i] + (p.bias != nullptr ? ld(p.bias + j + i) : 0.0f));
+        }
+        ptx::cluster_sync();  // nobody's memory goes away while it is read
+    }
+    if (warp == 1) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc(tmem_base, Tile::kTmemCols);
+    }
+}
+
+// Codes [rows][pitch bytes], boxes of 128 bytes (256 elements) x box_rows, 128-byte swizzle, zeros outside.
+bcq_status make_tmap_codes(CUtensorMap* m, const void* base, int rows, size_t pitch, int box_rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (fn == nullptr) {
+        set_last_cuda_error((int)cudaErrorNotSupported);
+        return BCQ_ERR_CUDA;
+    }
+    cuuint64_t dims[2] = {(cuuint64_t)pitch, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)pitch};
+    cuuint32_t box[2] = {128u, (cuuint32_t)box_rows};
+    cuuint32_t estr[2] = {1u, 1u};
+    CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        set_last_cuda_error((int)cudaErrorInvalidValue);
+        return BCQ_ERR_CUDA;
+    }
+    return BCQ_OK;
+}
+
+// Which tile, and how many CTAs share one.  Costs in cycles: a step of 256 elements is bound by shared memory, which
+// takes the step's codes once from memory and once to the tensor core at 128 bytes a cycle; an epilogue that nothing
+// hides; joining the partial sums of a cluster.
+struct MxPlan {
+    int bn, splits;
+};
+
+MxPlan plan_mx(int d_out, int atoms, int n) {
+    const int steps = ceil_div(atoms, 2), m_tiles = ceil_div(d_out, 128);
+    MxPlan best = {256, 1};
+    double least = 1e30;
+    // (tiles of fewer than 128 tokens only where one holds all: tokens' scales come in 128s)
+    for (int bn = n <= 16 ? 16 : n <= 32 ? 32 : n <= 64 ? 64 : 128; bn <= 256; bn *= 2) {
+        if (bn > 128 && n <= 128) break;
+        const int tiles = m_tiles * ceil_div(n, bn), slots = sm_count() * (bn <= 64 ? 2 : 1);
+        const double cycles = 2.0 * (128 + bn) * 128 / 128 * (bn <= 64 ? 2 : 1), tail = bn == 256 ? 900 : 400;
+        for (int s = 1; s <= 8 && s <= steps; ++s) {
+            if (s > 1 && tiles * s > slots) break;
+            const double cost = (double)ceil_div(tiles * s, slots) * (ceil_div(steps, s) * cycles + tail) + (s > 1 ? 1200 + 4.0 * bn : 0);
+            if (cost < least) {
+                least = cost;
+                best.bn = bn;
+                best.splits = s;
+            }
+        }
+    }
+    return best;
+}
+
+template <int BN, typename Out>
+bcq_status launch_mx(const CUtensorMap& tw, const CUtensorMap& tx, const MxLinearParams& p, cudaStream_t s) {
+    using Tile = MxTile<BN>;
+    const bcq_status st = ensure_dynamic_smem(mx_linear_kernel<BN, Out>, Tile::kSmem);
+    if (st != BCQ_OK) return st;
+    const int tiles = p.m_tiles * p.n_tiles;
+    const int ctas = p.splits > 1 ? tiles * p.splits : std::min(tiles, sm_count() * Tile::kPerSm);
+    BCQ_CUDA_TRY(launch_pdl(mx_linear_kernel<BN, Out>, dim3((unsigned)ctas), kThreads, Tile::kSmem, s, (unsigned)p.splits, tw, tx, p));
+    return BCQ_OK;
+}
+
+bcq_status check_mx(int rows, int cols, const void* codes, const void* scales) {
+    if (rows < 0 || cols < 1) return BCQ_ERR_SHAPE;
+    if (cols > kMxMaxCols) return BCQ_ERR_UNSUPPORTED;
+    if (rows == 0) return BCQ_OK;
+    if (!codes || !scales) return BCQ_ERR_NULL;
+    if (!aligned16(codes) || !aligned16(scales)) return BCQ_ERR_ALIGN;
+    return BCQ_OK;
+}
+
+bcq_status check_mx_values(int rows, int cols, const void* X, size_t ldx, int dtype) {
+    if (ldx < (size_t)cols) return BCQ_ERR_SHAPE;
+    if (dtype != BCQ_F32 && dtype != BCQ_BF16) return BCQ_ERR_UNSUPPORTED;
+    if (rows > 0 && !X) return BCQ_ERR_NULL;
+    if ((reinterpret_cast<uintptr_t>(X) & (dtype == BCQ_BF16 ? 1u : 3u)) != 0) return BCQ_ERR_ALIGN;
+    return BCQ_OK;
+}
+
+MxQuantParams mx_params(int rows, int cols, const void* X, size_t ldx, int dtype, int unit_rows) {
+    MxQuantParams p;
+    p.rows = rows; p.cols = cols; p.atoms = mx_atoms(cols);
+    p.vec = aligned16(X) && (ldx % (dtype == BCQ_BF16 ? 8 : 4)) == 0;
+    p.ld = (long long)ldx; p.pitch = (long long)mx_pitch(cols);
+    p.units = (long long)unit_rows * p.atoms;
+    return p;
+}
+
+unsigned mx_grid(long long units) {
+    const long long blocks = (units * 16 + 255) / 256;
+    return (unsigned)std::max(1ll, std::min(blocks, (long long)sm_count() * 8));
+}
+
+}  // namespace
+
+namespace bcq {
+bcq_status mx_timeout_flag(int* flag_out, int reset) {
+    int v = 0;
+    BCQ_CUDA_TRY(cudaMemcpyFromSymbol(&v, g_timeout_flag, sizeof(int)));
+    *flag_out = v;
+    if (reset && v != 0) {
+        const int zero = 0;
+        BCQ_CUDA_TRY(cudaMemcpyToSymbol(g_timeout_flag, &zero, sizeof(int)));
+    }
+    return BCQ_OK;
+}
+}  // namespace bcq
+
+extern "C" size_t bcq_mx_codes_bytes(int rows, int cols) { return rows < 1 || cols < 1 ? 0 : (size_t)rows * mx_pitch(cols); }
+
+extern "C" size_t bcq_mx_scales_bytes(int rows, int cols) {
+    return rows < 1 || cols < 1 ? 0 : (((size_t)rows + 127) / 128) * (size_t)mx_atoms(cols) * 512;
+}
+
+extern "C" bcq_status bcq_mx_quantize(int rows, int cols, const void* X, size_t ldx, int x_dtype, uint8_t* codes, uint8_t* scales,
+                                      void* stream) {
+    bcq_status st = check_mx(rows, cols, codes, scales);
+    if (st != BCQ_OK) return st;
+    if ((st = check_mx_values(rows, cols, X, ldx, x_dtype)) != BCQ_OK) return st;
+    if (rows == 0) return BCQ_OK;
+    const MxQuantParams p = mx_params(rows, cols, X, ldx, x_dtype, ceil_div(rows, 128) * 128);
+    cudaStream_t s = (cudaStream_t)stream;
+    uint32_t* sw = reinterpret_cast<uint32_t*>(scales);
+    if (x_dtype == BCQ_BF16)
+        BCQ_CUDA_TRY(launch_pdl(mx_quantize_kernel<__nv_bfloat16>, dim3(mx_grid(p.units)), 256, 0, s, 1, (const __nv_bfloat16*)X, codes, sw, p));
+    else
+        BCQ_CUDA_TRY(launch_pdl(mx_quantize_kernel<float>, dim3(mx_grid(p.units)), 256, 0, s, 1, (const float*)X, codes, sw, p));
+    return BCQ_OK;
+}
+
+extern "C" bcq_status bcq_mx_dequantize(int rows, int cols, const uint8_t* codes, const uint8_t* scales, void* X_hat, size_t ldx,
+                                        int x_dtype, void* stream) {
+    bcq_status st = check_mx(rows, cols, codes, scales);
+    if (st != BCQ_OK) return st;
+    if ((st = check_mx_values(rows, cols, X_hat, ldx, x_dtype)) != BCQ_OK) return st;
+    if (rows == 0) return BCQ_OK;
+    const MxQuantParams p = mx_params(rows, cols, X_hat, ldx, x_dtype, rows);
+    cudaStream_t s = (cudaStream_t)stream;
+    const uint32_t* sw = reinterpret_cast<const uint32_t*>(scales);
+    if (x_dtype == BCQ_BF16)
+        BCQ_CUDA_TRY(launch_pdl(mx_dequantize_kernel<__nv_bfloat16>, dim3(mx_grid(p.units)), 256, 0, s, 1, codes, sw, (__nv_bfloat16*)X_hat, p));
+    else
+        BCQ_CUDA_TRY(launch_pdl(mx_dequantize_kernel<float>, dim3(mx_grid(p.units)), 256, 0, s, 1, codes, sw, (float*)X_hat, p));
+    return BCQ_OK;
+}
+
+extern "C" bcq_status bcq_mx_linear(int d_out, int d_in, int n, const uint8_t* x_codes, const uint8_t* x_scales, const uint8_t* w_codes,
+                                    const uint8_t* w_scales, const float* bias, void* Y, size_t ldy, int y_dtype, void* stream) {
+    if (d_out < 1) return BCQ_ERR_SHAPE;
+    bcq_status st = check_mx(d_out, d_in, w_codes, w_scales);
+    if (st != BCQ_OK) return st;
+    if ((st = check_mx(n, d_in, x_codes, x_scales)) != BCQ_OK) return st;
+    if ((st = check_mx_values(n, d_out, Y, ldy, y_dtype)) != BCQ_OK) return st;
+    if ((reinterpret_cast<uintptr_t>(bias) & 3u) != 0) return BCQ_ERR_ALIGN;
+    if (n == 0) return BCQ_OK;
+    MxLinearParams p;
+    p.d_out = d_out; p.n = n; p.atoms = mx_atoms(d_in); p.steps = ceil_div(p.atoms, 2);
+    p.w_scales = w_scales; p.x_scales = x_scales; p.bias = bias; p.Y = Y; p.ldy = (long long)ldy;
+    const MxPlan plan = plan_mx(d_out, p.atoms, n);
+    p.splits = plan.splits;
+    p.m_tiles = ceil_div(d_out, 128); p.n_tiles = ceil_div(n, plan.bn);
+    CUtensorMap tw, tx;
+    if ((st = make_tmap_codes(&tw, w_codes, d_out, mx_pitch(d_in), 128)) != BCQ_OK) return st;
+    if ((st = make_tmap_codes(&tx, x_codes, n, mx_pitch(d_in), plan.bn)) != BCQ_OK) return st;
+    cudaStream_t s = (cudaStream_t)stream;
+    const bool bf16 = y_dtype == BCQ_BF16;
+    switch (plan.bn) {
+        case 16: return bf16 ? launch_mx<16, __nv_bfloat16>(tw, tx, p, s) : launch_mx<16, float>(tw, tx, p, s);
+        case 32: return bf16 ? launch_mx<32, __nv_bfloat16>(tw, tx, p, s) : launch_mx<32, float>(tw, tx, p, s);
+        case 64: return bf16 ? launch_mx<64, __nv_bfloat16>(tw, tx, p, s) : launch_mx<64, float>(tw, tx, p, s);
+        case 128: return bf16 ? launch_mx<128, __nv_bfloat16>(tw, tx, p, s) : launch_mx<128, float>(tw, tx, p, s);
+        default: return bf16 ? launch_mx<256, __nv_bfloat16>(tw, tx, p, s) : launch_mx<256, float>(tw, tx, p, s);
+    }
+}

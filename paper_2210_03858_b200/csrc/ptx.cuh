@@ -232,6 +232,80 @@ __device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
                  : "memory");
 }
 
+// ---------------------------------------------------------------- one CTA, and block-scaled products
+
+// 2-D tile load, and a copy of contiguous bytes (16-byte aligned, a multiple of 16), both counted on a barrier of this CTA.
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* m, int x, int y, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
+__device__ __forceinline__ void tmem_alloc(uint32_t holder_smem, uint32_t ncols) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(holder_smem), "r"(ncols) : "memory");
+}
+__device__ __forceinline__ void tmem_relinquish() {
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t ncols) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+}
+
+// Arrives on the barrier once every UMMA that this thread issued so far has completed.
+__device__ __forceinline__ void umma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// 32 rows of 16 bytes (512 contiguous bytes of shared memory) into four columns of tensor memory, once for each
+// quarter of its lanes: the place of 128 rows' scales, four scales of a row in a cell.  UMMAs that the same thread issues
+// afterwards see them.
+__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint32_t smem_addr) {
+    // descriptor without swizzle: groups of eight rows 128 bytes apart
+    const uint32_t lo = (smem_addr >> 4) & 0x3FFFu, hi = (128u >> 4) | (1u << 14);
+    asm volatile(
+        "{\n\t"
+        ".reg .b64 d;\n\t"
+        "mov.b64 d, {%1, %2};\n\t"
+        "tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], d;\n\t"
+        "}\n"
+        ::"r"(taddr), "r"(lo), "r"(hi)
+        : "memory");
+}
+
+// D[tmem] (+)= A B, both e2m1 with a power-of-two scale for every 32 elements of a row, whose places in tensor memory are
+// given: 64 elements of K.
+__device__ __forceinline__ void umma_mxf4(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                          uint32_t scale_a, uint32_t scale_b, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        ".reg .b64 da, db;\n\t"
+        "mov.b64 da, {%1, %2};\n\t"
+        "mov.b64 db, {%3, %4};\n\t"
+        "setp.ne.b32 p, %8, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %5, [%6], [%7], p;\n\t"
+        "}\n"
+        ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate)
+        : "memory");
+}
+
+// Instruction descriptor for kind::mxf4, e2m1 inputs (K-major), ue8m0 scales.  A cell of tensor memory holds the scales
+// of 128 elements; `pair` says which two of the four belong to this UMMA (0: the first 64 elements, 1: the second).
+__host__ __device__ constexpr uint32_t make_idesc_mxf4(int M, int N, int pair) {
+    return ((uint32_t)(2 * pair) << 4)         // scales of B: first of the two bytes
+           | (1u << 7) | (1u << 10)            // A, B: e2m1
+           | ((uint32_t)(N >> 3) << 17)
+           | (1u << 23)                        // scales: ue8m0
+           | ((uint32_t)(M >> 4) << 24)
+           | ((uint32_t)(2 * pair) << 29);     // scales of A
+}
+
 // ---------------------------------------------------------------- UMMA
 
 // Instruction descriptor for kind::f16 with bf16 inputs and fp32 accumulation.
