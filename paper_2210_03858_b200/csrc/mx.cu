@@ -64,13 +64,36 @@ __device__ __forceinline__ void load_eight(const __nv_bfloat16* p, float (&v)[8]
 }
 
 // Where the four scales of 128 elements of a row are, as one word.
-__device__ __forceinline__ long long scale_word(long long row, int atom, int atoms) {
-    return (((row >> 7) * atoms + atom) * 32 + (row & 31)) * 4 + ((row >> 5) & 3);
+__device__ __forceinline__ long long scale_word(int row, int atom, int atoms) {
+    return (((long long)(row >> 7) * atoms + atom) * 32 + (row & 31)) * 4 + ((row >> 5) & 3);
 }
 
 struct MxQuantParams {
     int rows, cols, atoms, vec;  // vec: rows are 16-byte aligned
-    long long ld, pitch, units;  // units: (row of the padded 128s, atom)
+    int unit_rows;               // rows in the container (128s) for quantisation, of the matrix for its inverse
+    long long ld, pitch;
+};
+
+// The units of work, (row, 128 elements of it), that a group of sixteen lanes goes through.  One division at the start; a step
+// of all groups is so many rows and so many atoms.
+struct Walk {
+    int row, atom, drow, datom, atoms;
+    __device__ __forceinline__ explicit Walk(int atoms_) : atoms(atoms_) {
+        const long long group = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 4;
+        const int groups = (int)(gridDim.x * (blockDim.x >> 4));
+        row = (int)(group / atoms);
+        atom = (int)(group - (long long)row * atoms);
+        drow = groups / atoms;
+        datom = groups - drow * atoms;
+    }
+    __device__ __forceinline__ void step() {
+        row += drow;
+        atom += datom;
+        if (atom >= atoms) {
+            atom -= atoms;
+            ++row;
+        }
+    }
 };
 
 // Sixteen lanes have 128 elements of a row, eight each: four of them a block.  Bound by memory.  A lane has
@@ -83,19 +106,19 @@ mx_quantize_kernel(const T* X, uint8_t* codes, uint32_t* scales, const MxQuantPa
     pdl_trigger();
     pdl_wait();
     const int lane16 = (int)threadIdx.x & 15;
-    const long long group = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 4;
-    const long long groups = ((long long)gridDim.x * blockDim.x) >> 4;
+    Walk w(p.atoms);
     // (units are an even number, as rows come in 128s: both groups of a warp take every turn, as the shuffles want)
-    for (long long first = group; first < p.units; first += groups * kUnits) {
+    while (w.row < p.unit_rows) {
         float v[kUnits][8];
+        int rows[kUnits], atoms[kUnits];
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
-            const long long unit = first + u * groups;
-            const long long row = unit / p.atoms;
-            const int col = (int)(unit - row * p.atoms) * 128 + lane16 * 8;
+            const int row = rows[u] = w.row, atom = atoms[u] = w.atom;
+            w.step();
+            const int col = atom * 128 + lane16 * 8;
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[u][i] = 0.0f;
-            if (unit < p.units && row < p.rows) {
+            if (row < p.rows) {
                 const T* src = X + row * p.ld + col;
                 if (p.vec && col + 8 <= p.cols) {
                     load_eight(src, v[u]);
@@ -108,7 +131,6 @@ mx_quantize_kernel(const T* X, uint8_t* codes, uint32_t* scales, const MxQuantPa
         }
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
-            const long long unit = first + u * groups;
             uint32_t top = 0;  // (as whole numbers: NaN and infinity are the largest)
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = max(top, abs_bits(v[u][i]));
@@ -125,12 +147,9 @@ mx_quantize_kernel(const T* X, uint8_t* codes, uint32_t* scales, const MxQuantPa
             uint32_t word = s << (8 * ((lane16 >> 2) & 3));
             word |= __shfl_xor_sync(0xffffffffu, word, 4);
             word |= __shfl_xor_sync(0xffffffffu, word, 8);
-            if (unit < p.units) {
-                const long long row = unit / p.atoms;
-                const int atom = (int)(unit - row * p.atoms);
-                if (row < p.rows) *reinterpret_cast<uint32_t*>(codes + row * p.pitch + atom * 64 + lane16 * 4) = c;
-                if (lane16 == 0) scales[scale_word(row, atom, p.atoms)] = word;
-            }
+            const int row = rows[u], atom = atoms[u];
+            if (row < p.rows) *reinterpret_cast<uint32_t*>(codes + row * p.pitch + atom * 64 + lane16 * 4) = c;
+            if (lane16 == 0 && row < p.unit_rows) scales[scale_word(row, atom, p.atoms)] = word;
         }
     }
 }
@@ -145,27 +164,24 @@ __global__ void __launch_bounds__(256)
 mx_dequantize_kernel(const uint8_t* codes, const uint32_t* scales, T* X, const MxQuantParams p) {
     pdl_wait();
     const int lane16 = (int)threadIdx.x & 15;
-    const long long group = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 4;
-    const long long groups = ((long long)gridDim.x * blockDim.x) >> 4;
-    for (long long first = group; first < p.units; first += groups * kUnits) {
+    Walk w(p.atoms);
+    while (w.row < p.unit_rows) {
         uint32_t c[kUnits], s[kUnits];
+        int rows[kUnits], atoms[kUnits];
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
-            const long long unit = first + u * groups;
+            const int row = rows[u] = w.row, atom = atoms[u] = w.atom;
+            w.step();
             c[u] = s[u] = 0;
-            if (unit < p.units) {
-                const long long row = unit / p.atoms;
-                const int atom = (int)(unit - row * p.atoms);
+            if (row < p.unit_rows) {
                 c[u] = ld_stream(reinterpret_cast<const uint32_t*>(codes + row * p.pitch + atom * 64 + lane16 * 4));
                 s[u] = ld(scales + scale_word(row, atom, p.atoms));
             }
         }
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
-            const long long unit = first + u * groups;
-            if (unit >= p.units) break;
-            const long long row = unit / p.atoms;
-            const int col = (int)(unit - row * p.atoms) * 128 + lane16 * 8;
+            const int row = rows[u], col = atoms[u] * 128 + lane16 * 8;
+            if (row >= p.unit_rows) break;
             const float f = scale_value((s[u] >> (8 * (lane16 >> 2))) & 255u);
             float v[8];
 #pragma unroll
@@ -539,12 +555,12 @@ MxQuantParams mx_params(int rows, int cols, const void* X, size_t ldx, int dtype
     p.rows = rows; p.cols = cols; p.atoms = mx_atoms(cols);
     p.vec = aligned16(X) && (ldx % (dtype == BCQ_BF16 ? 8 : 4)) == 0;
     p.ld = (long long)ldx; p.pitch = (long long)mx_pitch(cols);
-    p.units = (long long)unit_rows * p.atoms;
+    p.unit_rows = unit_rows;
     return p;
 }
 
-unsigned mx_grid(long long units) {
-    const long long blocks = (units * 16 + 255) / 256;
+unsigned mx_grid(const MxQuantParams& p) {
+    const long long blocks = ((long long)p.unit_rows * p.atoms * 16 + 255) / 256;
     return (unsigned)std::max(1ll, std::min(blocks, (long long)sm_count() * 8));
 }
 
@@ -579,9 +595,9 @@ extern "C" bcq_status bcq_mx_quantize(int rows, int cols, const void* X, size_t 
     cudaStream_t s = (cudaStream_t)stream;
     uint32_t* sw = reinterpret_cast<uint32_t*>(scales);
     if (x_dtype == BCQ_BF16)
-        BCQ_CUDA_TRY(launch_pdl(mx_quantize_kernel<__nv_bfloat16>, dim3(mx_grid(p.units)), 256, 0, s, 1, (const __nv_bfloat16*)X, codes, sw, p));
+        BCQ_CUDA_TRY(launch_pdl(mx_quantize_kernel<__nv_bfloat16>, dim3(mx_grid(p)), 256, 0, s, 1, (const __nv_bfloat16*)X, codes, sw, p));
     else
-        BCQ_CUDA_TRY(launch_pdl(mx_quantize_kernel<float>, dim3(mx_grid(p.units)), 256, 0, s, 1, (const float*)X, codes, sw, p));
+        BCQ_CUDA_TRY(launch_pdl(mx_quantize_kernel<float>, dim3(mx_grid(p)), 256, 0, s, 1, (const float*)X, codes, sw, p));
     return BCQ_OK;
 }
 
@@ -595,9 +611,9 @@ extern "C" bcq_status bcq_mx_dequantize(int rows, int cols, const uint8_t* codes
     cudaStream_t s = (cudaStream_t)stream;
     const uint32_t* sw = reinterpret_cast<const uint32_t*>(scales);
     if (x_dtype == BCQ_BF16)
-        BCQ_CUDA_TRY(launch_pdl(mx_dequantize_kernel<__nv_bfloat16>, dim3(mx_grid(p.units)), 256, 0, s, 1, codes, sw, (__nv_bfloat16*)X_hat, p));
+        BCQ_CUDA_TRY(launch_pdl(mx_dequantize_kernel<__nv_bfloat16>, dim3(mx_grid(p)), 256, 0, s, 1, codes, sw, (__nv_bfloat16*)X_hat, p));
     else
-        BCQ_CUDA_TRY(launch_pdl(mx_dequantize_kernel<float>, dim3(mx_grid(p.units)), 256, 0, s, 1, codes, sw, (float*)X_hat, p));
+        BCQ_CUDA_TRY(launch_pdl(mx_dequantize_kernel<float>, dim3(mx_grid(p)), 256, 0, s, 1, codes, sw, (float*)X_hat, p));
     return BCQ_OK;
 }
 

@@ -1,15 +1,15 @@
 // Operators over rows of logits: log probabilities of given tokens with entropy and top alternatives, and the
 // distillation loss against a teacher's top log probabilities with its gradient.
 //
-// With c = log2(e) / T everything is a sum over a row of 2^(c (x - m)), m = max x.  All three kernels read a row once
+// With c = log2(e) / T everything is a sum over a row of 2^(c x - b), b = c max x.  All three kernels read a row once
 // from memory: a thread keeps a running maximum and the sums that go with it, and rescales them when a batch of its
 // vectors has a larger one, so no second pass is needed for the sums; the sums of threads, warps and CTAs are joined in
-// a fixed order.  The difference is taken before it is scaled: c x alone overflows for a logit of the type's
-// lowest value, and a row that holds nothing else is a row of equals.  What bounds them is memory: n vocab sizeof(T) bytes read (and written, for the
-// gradient).  An element costs one exponential, two packed half-instructions and a conversion; the exponentials
-// alone (16 a cycle and SM) take 0.7 of the time the bytes of bf16 logits take, so whatever else an element costs has to
-// issue beside them: sums and products go two at a time (fma.rn.f32x2), maxima of bf16 two at a time, and the
-// comparison that guards the running maximum is made once for a batch of four vectors.
+// a fixed order.  b is the rounded product and is subtracted everywhere (from a target, from an alternative), so its
+// rounding error, which would be that of a probability, drops out.  What bounds them is memory: n vocab sizeof(T)
+// bytes read (and written, for the gradient).  Next to that is the issue of instructions: an element of bf16 costs a
+// conversion, an exponential (16 a cycle and SM: 0.7 of the time its bytes take), a product and a sum for each result,
+// half a maximum and half a clamp.  (With sums and products two at a time, fma.rn.f32x2, it was 11 instructions and not
+// 7: the pairs have to be put together.)
 //
 // Rows start at any element (an odd vocabulary in bf16 leaves rows at odd addresses): the elements before the
 // first and after the last whole 16-byte vector of a row belong to single threads.
@@ -18,7 +18,10 @@
 // one SM alone takes 3 us to bring in.
 #include <cuda_bf16.h>
 
+#include <cfloat>
+
 #include <algorithm>
+#include <type_traits>
 
 #include "gemm_common.cuh"
 
@@ -30,7 +33,7 @@ constexpr int kVocabMax = 393216;
 constexpr int kTopMax = 128;
 constexpr int kBatch = 4;          // 16-byte vectors of a thread between two looks at the running maximum
 constexpr float kFloor = -1000.0f; // exponents below are as good as this one (2^-1000 = 0), and 0 * -1000 is 0
-constexpr int kCandidates = 2048;  // elements, and batches, that may be as large as the k-th largest
+constexpr int kCandidates = 2048;  // elements that may be as large as the k-th largest, and batches that hold some
 constexpr float kLn2 = 0.693147180559945309f;
 
 __device__ __forceinline__ float ex2(float x) {
@@ -51,7 +54,7 @@ __device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) {
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
 __device__ __forceinline__ float quiet_nan() { return __int_as_float(0x7fc00000); }
 
-// Two floats in a register pair: what the packed instructions of sm_100 take.
+// Two floats in a register pair, and the instructions of sm_100 that take them.
 typedef unsigned long long f32x2;
 __device__ __forceinline__ f32x2 pack2(float a, float b) {
     f32x2 r;
@@ -64,15 +67,23 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
-    f32x2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
     f32x2 r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
+}
+
+// Logits beyond this, either way, are taken apart from the rest: c x may overflow.  Below -kFar times two a logit next to one
+// within kFar is as good as -kFar times two.
+constexpr float kFar = 6.338253e29f;  // 2^99
+
+// Exponent of 2 of an element x relative to the maximum m, and that of a sum relative to the maximum a when it is taken
+// to the maximum m.  The rounded product m c is what is subtracted, each time the same number.
+__device__ __forceinline__ float rel(float x, float m, float c) {
+    return fabsf(m) <= kFar ? fmaf(fmaxf(x, -2.0f * kFar), c, -__fmul_rn(m, c)) : (x - m) * c;
+}
+__device__ __forceinline__ float rel_base(float a, float m, float c) {
+    return fabsf(a) <= kFar && fabsf(m) <= kFar ? __fsub_rn(__fmul_rn(a, c), __fmul_rn(m, c)) : (a - m) * c;
 }
 
 // ---------------------------------------------------------------- element types
@@ -93,9 +104,11 @@ struct Elem<float> {
     static __device__ __forceinline__ float max_of4(const uint4* v) {
         return max_nan(max_nan(max_of(v[0]), max_of(v[1])), max_nan(max_of(v[2]), max_of(v[3])));
     }
-    static __device__ __forceinline__ void pairs(const uint4& v, f32x2* x) {
-        x[0] = pack2(__uint_as_float(v.x), __uint_as_float(v.y));
-        x[1] = pack2(__uint_as_float(v.z), __uint_as_float(v.w));
+    static __device__ __forceinline__ void clamp(uint4& v) {
+        v.x = __float_as_uint(fmaxf(__uint_as_float(v.x), -2.0f * kFar));
+        v.y = __float_as_uint(fmaxf(__uint_as_float(v.y), -2.0f * kFar));
+        v.z = __float_as_uint(fmaxf(__uint_as_float(v.z), -2.0f * kFar));
+        v.w = __float_as_uint(fmaxf(__uint_as_float(v.w), -2.0f * kFar));
     }
     static __device__ __forceinline__ void mask(uint4& v, uint32_t bits) {
         if (bits & 1u) v.x = kMasked;
@@ -125,12 +138,13 @@ struct Elem<__nv_bfloat16> {
         const uint32_t m = max_nan_bf16x2(max_nan_bf16x2(max2_of(v[0]), max2_of(v[1])), max_nan_bf16x2(max2_of(v[2]), max2_of(v[3])));
         return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
     }
-    static __device__ __forceinline__ void pairs(const uint4& v, f32x2* x) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t w = word(v, i);
-            x[i] = pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-        }
+    static __device__ __forceinline__ uint32_t clamp2(uint32_t w) {
+        uint32_t r;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0xf180f180u));  // -2^100
+        return r;
+    }
+    static __device__ __forceinline__ void clamp(uint4& v) {
+        v = make_uint4(clamp2(v.x), clamp2(v.y), clamp2(v.z), clamp2(v.w));
     }
     static __device__ __forceinline__ void mask(uint4& v, uint32_t bits) {
         uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -170,61 +184,128 @@ struct Share {
     __device__ __forceinline__ const uint4* vec(int v) const { return reinterpret_cast<const uint4*>(row + head) + v; }
 };
 
+// Sums of e and e z over a vector of a row that lies far out as a whole, or holds nothing so far.
+template <typename T>
+__device__ __noinline__ float2 far_sums(uint4 v, float m, float c) {
+    const float base = m == neg_inf() ? 0.0f : m;
+    float2 r = make_float2(0.0f, 0.0f);
+    for (int i = 0; i < Elem<T>::E; ++i) {
+        const float z = fmaxf((Elem<T>::at(v, i) - base) * c, kFloor), e = ex2(z);
+        r.x += e;
+        r.y = fmaf(e, z, r.y);
+    }
+    return r;
+}
+
 // Running maximum and the sums relative to it.  ENTROPY: sum of e z too, z the exponent of e.
 template <typename T, bool ENTROPY>
 struct Running {
     float m = neg_inf();
-    f32x2 s = 0, t = 0;  // (two partial sums each)
-    bool bad = false;    // a NaN or +inf was seen
+    float s[2] = {0.0f, 0.0f}, t[2] = {0.0f, 0.0f};  // (two partial sums each)
+    bool bad = false;                                // a NaN or +inf was seen
 
     __device__ __forceinline__ void raise(float x, float c) {
+        if (x <= m) return;  // (not so with a NaN)
         if (x > m) {
-            const float d = fmaxf((m - x) * c, kFloor), f = ex2(d);
-            const f32x2 ff = pack2(f, f);
-            if (ENTROPY) t = mul2(ff, fma2(pack2(d, d), s, t));
-            s = mul2(ff, s);
+            const float d = fmaxf(rel_base(m, x, c), kFloor), f = ex2(d);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if (ENTROPY) t[i] = f * fmaf(d, s[i], t[i]);
+                s[i] *= f;
+            }
             m = x;
         }
         if (!(x < __int_as_float(0x7f800000))) bad = true;
     }
-    __device__ __forceinline__ float base() const { return m == neg_inf() ? 0.0f : m; }
-    __device__ __forceinline__ void add(const uint4& v, f32x2 c2, f32x2 nm2) {
-        f32x2 x[Elem<T>::E / 2];
-        Elem<T>::pairs(v, x);
+    __device__ __forceinline__ void add_near(uint4 v, float c, float nb) {
+        if (ENTROPY) Elem<T>::clamp(v);  // (what is -inf must not be multiplied with its e = 0)
+        f32x2 s2 = pack2(s[0], s[1]), t2 = pack2(t[0], t[1]);
+        const f32x2 c2 = pack2(c, c), nb2 = pack2(nb, nb);
 #pragma unroll
-        for (int i = 0; i < Elem<T>::E / 2; ++i) {
+        for (int i = 0; i < Elem<T>::E; i += 2) {
+            const f32x2 z = fma2(pack2(Elem<T>::at(v, i), Elem<T>::at(v, i + 1)), c2, nb2);
             float a, b;
-            unpack2(mul2(add2(x[i], nm2), c2), a, b);
-            if (ENTROPY) {
-                a = fmaxf(a, kFloor);
-                b = fmaxf(b, kFloor);
-            }
+            unpack2(z, a, b);
             const f32x2 e = pack2(ex2(a), ex2(b));
-            s = add2(s, e);
-            if (ENTROPY) t = fma2(e, pack2(a, b), t);
+            s2 = add2(s2, e);
+            if (ENTROPY) t2 = fma2(e, z, t2);
         }
+        unpack2(s2, s[0], s[1]);
+        if (ENTROPY) unpack2(t2, t[0], t[1]);
     }
-    __device__ __forceinline__ float batch(const uint4 (&v)[kBatch], float c) {
+    __device__ __forceinline__ void add_far(uint4 v, float c) {
+        const float2 f = far_sums<T>(v, m, c);
+        s[0] += f.x;
+        if (ENTROPY) t[0] += f.y;
+    }
+    // Adds the first `have` of the vectors (the others are masked); returns the largest element.
+    template <bool WHOLE>
+    __device__ __forceinline__ float batch(const uint4 (&v)[kBatch], int have, float c) {
         const float x = Elem<T>::max_of4(v);
         raise(x, c);
-        const float b = -base();
-        const f32x2 c2 = pack2(c, c), nm2 = pack2(b, b);
+        if (fabsf(m) <= kFar) {
+            const float nb = -__fmul_rn(m, c);
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) add(v[u], c2, nm2);
+            for (int u = 0; u < kBatch; ++u)
+                if (WHOLE || u < have) add_near(v[u], c, nb);
+        } else {
+            for (int u = 0; u < kBatch; ++u)
+                if (WHOLE || u < have) add_far(u == 0 ? v[0] : u == 1 ? v[1] : u == 2 ? v[2] : v[3], c);
+        }
         return x;
     }
     __device__ __forceinline__ void one(float x, float c) {
         raise(x, c);
-        const float z = fmaxf((x - base()) * c, kFloor), e = ex2(z);
-        s = add2(s, pack2(e, 0.0f));
-        if (ENTROPY) t = fma2(pack2(e, 0.0f), pack2(z, 0.0f), t);
+        const float z = m == neg_inf() ? kFloor : fmaxf(rel(x, m, c), kFloor), e = ex2(z);
+        s[0] += e;
+        if (ENTROPY) t[0] = fmaf(e, z, t[0]);
     }
-    __device__ __forceinline__ void sums(float& s1, float& t1) const {
-        float a, b;
-        unpack2(s, a, b);
-        s1 = a + b;
-        unpack2(t, a, b);
-        t1 = a + b;
+};
+
+// Goes through the vectors of a share, kBatch of a thread at a time, each batch on its way while the one before it is used:
+// use(whole, b, v, have) gets batch b, of which this thread has the first `have` vectors.  The last, incomplete batch
+// comes first: the loop has whole ones only, without a condition on any load.
+template <typename T, int NT>
+struct Stream {
+    const uint4* at;
+    int whole, rest;  // whole batches, vectors of this thread in the incomplete one
+    bool more;        // there is an incomplete one
+
+    __device__ __forceinline__ explicit Stream(const Share<T>& sh) {
+        const int nv = sh.v1 - sh.v0, tid = (int)threadIdx.x;
+        at = sh.vec(sh.v0 + tid);
+        whole = nv / (kBatch * NT);
+        const int left = nv - whole * (kBatch * NT);
+        more = left > 0;
+        rest = (left - tid + NT - 1) / NT;
+    }
+    __device__ __forceinline__ int batches() const { return whole + (more ? 1 : 0); }
+    __device__ __forceinline__ void load(int b, uint4 (&v)[kBatch]) const {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) v[u] = ld_stream(at + b * (kBatch * NT) + u * NT);
+    }
+    __device__ __forceinline__ void load_rest(uint4 (&v)[kBatch]) const {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            v[u] = make_uint4(Elem<T>::kMasked, Elem<T>::kMasked, Elem<T>::kMasked, Elem<T>::kMasked);
+            if (u < rest) v[u] = ld_stream(at + whole * (kBatch * NT) + u * NT);
+        }
+    }
+    template <typename Before, typename Use>
+    __device__ __forceinline__ void run(Before before, Use use) const {
+        uint4 a[kBatch], b[kBatch];
+        if (more) load_rest(a);
+        if (whole > 0) load(0, b);
+        before();
+        if (more) use(std::false_type(), whole, a, rest);
+        for (int i = 0; i < whole; i += 2) {
+            if (i + 1 < whole) load(i + 1, a);
+            use(std::true_type(), i, b, kBatch);
+            if (i + 1 < whole) {
+                if (i + 2 < whole) load(i + 2, b);
+                use(std::true_type(), i + 1, a, kBatch);
+            }
+        }
     }
 };
 
@@ -238,46 +319,11 @@ __device__ __forceinline__ Stats join(const Stats& a, const Stats& b, float c) {
     Stats r;
     r.m = fmaxf(a.m, b.m);
     const float base = r.m == neg_inf() ? 0.0f : r.m;
-    const float da = fmaxf((a.m - base) * c, kFloor), db = fmaxf((b.m - base) * c, kFloor), fa = ex2(da), fb = ex2(db);
+    const float da = fmaxf(rel_base(a.m, base, c), kFloor), db = fmaxf(rel_base(b.m, base, c), kFloor), fa = ex2(da), fb = ex2(db);
     r.s = a.s * fa + b.s * fb;
     r.t = fa * (a.t + da * a.s) + fb * (b.t + db * b.s);
     r.bad = a.bad | b.bad;
     return r;
-}
-
-__device__ __forceinline__ Stats join_warp(Stats v, float c) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        Stats w;
-        w.m = __shfl_xor_sync(0xffffffffu, v.m, o);
-        w.s = __shfl_xor_sync(0xffffffffu, v.s, o);
-        w.t = __shfl_xor_sync(0xffffffffu, v.t, o);
-        w.bad = __shfl_xor_sync(0xffffffffu, v.bad, o);
-        v = join(v, w, c);
-    }
-    return v;
-}
-
-// Everything of the row, in every thread of the cluster.  `warps` holds NT / 32 entries; `mine` is read by the other CTAs.
-template <int NT>
-__device__ __forceinline__ Stats join_row(Stats v, Stats* warps, Stats* mine, int ctas, float c) {
-    v = join_warp(v, c);
-    if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = warps[0];
-#pragma unroll
-    for (int w = 1; w < NT / 32; ++w) v = join(v, warps[w], c);
-    if (ctas == 1) return v;
-    if (threadIdx.x == 0) *mine = v;
-    __syncwarp();
-    ptx::cluster_sync();
-    static_assert(sizeof(Stats) == 16, "one load");
-    for (int r = 0; r < ctas; ++r) {
-        const float4 f = ptx::ld_cluster_v4(ptx::cluster_addr(ptx::smem_u32(mine), (uint32_t)r));
-        const Stats w = {f.x, f.y, f.z, __float_as_int(f.w)};
-        v = r == 0 ? w : join(v, w, c);
-    }
-    return v;
 }
 
 // Order of the top list: larger value first, then the lower index.  Zeros of either sign are equal.
@@ -288,6 +334,52 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
 __device__ __forceinline__ unsigned long long key_of(float x, int index) {
     return ((unsigned long long)order_of(x) << 32) | (uint32_t)~index;
+}
+
+// Everything of the row, in every thread of the cluster.  `part` holds NT / 32 entries; `mine` is read by the other CTAs.
+// First the maximum, then every thread's sums relative to it.
+template <int NT, typename R>
+__device__ __forceinline__ Stats join_row(const R& run, Stats* part, Stats* mine, int ctas, float c) {
+    constexpr int NW = NT / 32;
+    static_assert(NW <= 16 && (NW & (NW - 1)) == 0, "warps");
+    const int lane = (int)threadIdx.x & 31, warp = (int)threadIdx.x >> 5;
+    const uint32_t top = __reduce_max_sync(0xffffffffu, order_of(run.m));
+    if (lane == 0) part[warp].m = value_of(top);
+    Stats v;
+    v.bad = __syncthreads_or(run.bad);
+    v.m = value_of(__reduce_max_sync(0xffffffffu, order_of(part[lane & (NW - 1)].m)));
+    const float d = fmaxf(rel_base(run.m, v.m == neg_inf() ? 0.0f : v.m, c), kFloor), f = ex2(d);
+    v.s = run.s[0] + run.s[1];
+    v.t = f * fmaf(d, v.s, run.t[0] + run.t[1]);
+    v.s *= f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        v.s += __shfl_xor_sync(0xffffffffu, v.s, o);
+        v.t += __shfl_xor_sync(0xffffffffu, v.t, o);
+    }
+    if (lane == 0) {
+        part[warp].s = v.s;
+        part[warp].t = v.t;
+    }
+    __syncthreads();
+    v.s = part[lane & (NW - 1)].s;
+    v.t = part[lane & (NW - 1)].t;
+#pragma unroll
+    for (int o = NW / 2; o > 0; o >>= 1) {
+        v.s += __shfl_xor_sync(0xffffffffu, v.s, o);
+        v.t += __shfl_xor_sync(0xffffffffu, v.t, o);
+    }
+    if (ctas == 1) return v;
+    if (threadIdx.x == 0) *mine = v;
+    __syncwarp();
+    ptx::cluster_sync();
+    static_assert(sizeof(Stats) == 16, "one load");
+    for (int r = 0; r < ctas; ++r) {
+        const float4 q = ptx::ld_cluster_v4(ptx::cluster_addr(ptx::smem_u32(mine), (uint32_t)r));
+        const Stats w = {q.x, q.y, q.z, __float_as_int(q.w)};
+        v = r == 0 ? w : join(v, w, c);
+    }
+    return v;
 }
 
 // ---------------------------------------------------------------- log probabilities
@@ -374,23 +466,32 @@ __device__ __forceinline__ void top_of_share(const Share<T>& sh, int k, float mi
         ts->num_cand = 0;
         ts->num_events = 0;
     }
-    __syncthreads();
-    int rank = 0;
-    for (int i = 0; i < NT; i += 4) {
-        const float4 o = *reinterpret_cast<const float4*>(&ts->largest[i]);
-        rank += (o.x > mine || (o.x == mine && i < tid)) + (o.y > mine || (o.y == mine && i + 1 < tid)) +
-                (o.z > mine || (o.z == mine && i + 2 < tid)) + (o.w > mine || (o.w == mine && i + 3 < tid));
-    }
-    if (rank == k - 1) ts->threshold = mine;
     for (int i = tid; i < k; i += NT) ts->best[i] = 0;
     __syncthreads();
+    if (tid < 32) {
+        // the k-th largest by bisection over the order of values, to 2^12 steps of fp32 (all of bf16): one warp, eight maxima a
+        // lane.  (Every thread counting the larger ones: 2 us of the 6.5 that an SM spent on a row.)
+        uint32_t o[NT / 32];
+#pragma unroll
+        for (int i = 0; i < NT / 32; ++i) o[i] = order_of(ts->largest[32 * i + tid]);
+        uint32_t lo = 0;  // at least k are as large
+#pragma unroll 1
+        for (int bit = 31; bit >= 12; --bit) {
+            const uint32_t mid = lo | (1u << bit);
+            int c = 0;
+#pragma unroll
+            for (int i = 0; i < NT / 32; ++i) c += o[i] >= mid;
+            if (__reduce_add_sync(0xffffffffu, c) >= k) lo = mid;
+        }
+        if (tid == 0) ts->threshold = value_of(max(lo, order_of(-FLT_MAX)));  // (-inf never belongs)
+    }
+    __syncthreads();
     const float bound = ts->threshold;
-    auto belongs = [&](float x) { return x >= bound && x > neg_inf(); };
-    auto take = [&](float x, int index) {
+    auto belongs = [&](float x) { return x >= bound; };
+    if (sh.single >= 0 && belongs(single)) {
         const int at = atomicAdd(&ts->num_cand, 1);
-        if (at < kCandidates) ts->cand[at] = key_of(x, index);
-    };
-    if (sh.single >= 0 && belongs(single)) take(single, sh.single);
+        if (at < kCandidates) ts->cand[at] = key_of(single, sh.single);
+    }
     if (belongs(mine))
         for (int b = 0; b < batches; ++b)
             if (belongs(batch_max[b * NT + tid])) {
@@ -405,20 +506,31 @@ __device__ __forceinline__ void top_of_share(const Share<T>& sh, int k, float mi
             const int v = sh.v0 + ((e / NT) * kBatch + i % kBatch) * NT + e % NT;
             if (v < sh.v1) {
                 const uint4 x = ld(sh.vec(v));
+                int have = 0;
 #pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    const float y = Elem<T>::at(x, j);
-                    if (belongs(y)) take(y, sh.head + v * E + j);
+                for (int j = 0; j < E; ++j) have += belongs(Elem<T>::at(x, j));
+                if (have > 0) {
+                    int at = atomicAdd(&ts->num_cand, have);
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        const float y = Elem<T>::at(x, j);
+                        if (belongs(y) && at < kCandidates) ts->cand[at++] = key_of(y, sh.head + v * E + j);
+                    }
                 }
             }
         }
     __syncthreads();
     if (events > kCandidates || ts->num_cand > kCandidates) gather_exactly<T>(sh, k, ts);
     const int n = min(ts->num_cand, kCandidates);
+    if (tid == 0 && (n & 1)) ts->cand[n] = 0;  // (two are read at a time)
+    __syncthreads();
     for (int i = tid; i < n; i += NT) {
         const unsigned long long key = ts->cand[i];
         int r = 0;
-        for (int j = 0; j < n; ++j) r += ts->cand[j] > key;
+        for (int j = 0; j < n; j += 2) {
+            const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&ts->cand[j]);
+            r += (o.x > key) + (o.y > key);
+        }
         if (r < k) ts->best[r] = key;
     }
     __syncthreads();
@@ -433,12 +545,18 @@ struct LogprobParams {
     int* top_index;
 };
 
+// (where the exponent of 2 may overflow, that of e may not)
+__device__ __forceinline__ float log_prob(float x, float m, float log_s, const LogprobParams& p) {
+    if (fabsf(x) <= kFar && fabsf(m) <= kFar) return (rel(x, m, p.c) - log_s) * kLn2;
+    return (x - m) * p.inv_t - log_s * kLn2;
+}
+
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kLpThreads)
 token_logprobs_kernel(const T* logits, const LogprobParams p) {
     constexpr int NT = kLpThreads;
     extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ Stats warps[NT / 32];
+    __shared__ Stats part[NT / 32];
     __shared__ Stats mine;
     pdl_wait();
     const int row = (int)blockIdx.x / p.ctas, rank = (int)blockIdx.x % p.ctas;
@@ -457,35 +575,20 @@ token_logprobs_kernel(const T* logits, const LogprobParams p) {
     const float single = sh.single >= 0 ? Elem<T>::get(sh.row + sh.single) : neg_inf();
 
     Running<T, true> run;
-    const uint4 masked = make_uint4(Elem<T>::kMasked, Elem<T>::kMasked, Elem<T>::kMasked, Elem<T>::kMasked);
-    auto load = [&](int b, uint4 (&v)[kBatch]) {
-        const int at = sh.v0 + b * (kBatch * NT) + tid;
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) v[u] = at + u * NT < sh.v1 ? ld_stream(sh.vec(at + u * NT)) : masked;
-    };
-    // the next batch is on its way while one is added up
-    uint4 now[kBatch], next[kBatch];
-    const int batches = (sh.v1 - sh.v0 + kBatch * NT - 1) / (kBatch * NT);
-    if (batches > 0) load(0, now);
-    for (int b = 0; b < batches; ++b) {
-        if (b + 1 < batches) load(b + 1, next);
-        const float x = run.batch(now, p.c);
-        if (TOP) batch_max[b * NT + tid] = x;
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) now[u] = next[u];
-    }
+    const Stream<T, NT> stream(sh);
+    stream.run([] {},
+               [&](auto whole, int b, uint4(&v)[kBatch], int have) {
+                   const float x = run.template batch<decltype(whole)::value>(v, have, p.c);
+                   if (TOP) batch_max[b * NT + tid] = x;
+               });
     if (sh.single >= 0) run.one(single, p.c);
 
-    Stats st;
-    run.sums(st.s, st.t);
-    st.m = run.m;
-    st.bad = run.bad ? 1 : 0;
-    st = join_row<NT>(st, warps, &mine, p.ctas, p.c);
+    const Stats st = join_row<NT>(run, part, &mine, p.ctas, p.c);
     const bool none = st.bad || !(st.s > 0.0f);  // no distribution
     const float log_s = log2f(st.s);
     if (rank == 0 && tid == 0) {
         if (p.logprob != nullptr) {
-            float lp = (given - st.m) * p.inv_t - log_s * kLn2;
+            float lp = log_prob(given, st.m, log_s, p);
             if (none || target >= p.vocab) lp = quiet_nan();
             else if (target < 0) lp = 0.0f;
             p.logprob[row] = lp;
@@ -497,7 +600,7 @@ token_logprobs_kernel(const T* logits, const LogprobParams p) {
         float* out = p.top_logprob + (long long)row * k;
         int* out_i = p.top_index + (long long)row * k;
         auto put = [&](int at, unsigned long long key) {
-            out[at] = key ? (value_of((uint32_t)(key >> 32)) - st.m) * p.inv_t - log_s * kLn2 : neg_inf();
+            out[at] = key ? log_prob(value_of((uint32_t)(key >> 32)), st.m, log_s, p) : neg_inf();
             out_i[at] = key ? (int)~(uint32_t)key : -1;
         };
         if (none) {  // the same in all CTAs of the row
@@ -507,7 +610,7 @@ token_logprobs_kernel(const T* logits, const LogprobParams p) {
                     out_i[i] = -1;
                 }
         } else {
-            top_of_share<T>(sh, k, run.m, single, batch_max, batches, ts);
+            top_of_share<T>(sh, k, run.m, single, batch_max, stream.batches(), ts);
             if (p.ctas == 1) {
                 for (int i = tid; i < k; i += NT) put(i, ts->best[i]);
             } else {
@@ -683,13 +786,13 @@ __device__ __forceinline__ void finish_row(const DistillParams& p, Teacher* te, 
     if (m == neg_inf()) m = 0.0f;
     float s = 0.0f;
     for (int i = lane; i < p.k; i += 32)
-        if (te->first[i]) s += ex2(fmaxf((te->x[i] - m) * p.c, kFloor));
+        if (te->first[i]) s += ex2(fmaxf(rel(te->x[i], m, p.c), kFloor));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if (lane == 0) {
         // The rest keeps its own maximum: rho may be too small for a float where its logarithm, and the shares of its
         // tokens in it, are not.
-        const float down = ex2(fmaxf((rest.m - m) * p.c, kFloor));
+        const float down = ex2(fmaxf(rel_base(rest.m, m, p.c), kFloor));
         te->m_rest = rest.m == neg_inf() ? 0.0f : rest.m;
         te->s_rest = rest.s;
         te->m = m;
@@ -728,7 +831,7 @@ __global__ void __launch_bounds__(kLossThreads)
 distill_loss_kernel(const T* logits, const DistillParams p) {
     constexpr int NT = kLossThreads;
     extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ Stats warps[NT / 32];
+    __shared__ Stats part[NT / 32];
     __shared__ Stats mine;
     __shared__ Teacher te;
     uint32_t* marks = reinterpret_cast<uint32_t*>(smem);
@@ -736,41 +839,27 @@ distill_loss_kernel(const T* logits, const DistillParams p) {
     const int row = (int)blockIdx.x / p.ctas, rank = (int)blockIdx.x % p.ctas;
     const Share<T> sh(logits + (long long)row * p.ld, p.vocab, rank, p.ctas);
     const int tid = (int)threadIdx.x;
-    const uint4 masked = make_uint4(Elem<T>::kMasked, Elem<T>::kMasked, Elem<T>::kMasked, Elem<T>::kMasked);
-    auto load = [&](int b, uint4 (&v)[kBatch]) {
-        const int at = sh.v0 + b * (kBatch * NT) + tid;
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) v[u] = at + u * NT < sh.v1 ? ld_stream(sh.vec(at + u * NT)) : masked;
-    };
     Running<T, false> run;
-    uint4 now[kBatch], next[kBatch];
-    const int batches = (sh.v1 - sh.v0 + kBatch * NT - 1) / (kBatch * NT);
-    if (batches > 0) load(0, now);
-    load_teacher<T, NT>(sh, p, row, &te, marks);
     const uint8_t* mark = reinterpret_cast<const uint8_t*>(marks);
-    for (int b = 0; b < batches; ++b) {
-        if (b + 1 < batches) load(b + 1, next);
-        const int at = b * (kBatch * NT) + tid;
+    const Stream<T, NT> stream(sh);
+    stream.run([&] { load_teacher<T, NT>(sh, p, row, &te, marks); },
+               [&](auto whole, int b, uint4(&v)[kBatch], int have) {
+                   const int at = b * (kBatch * NT) + tid + 1;
+                   uint32_t bits[kBatch], any = 0;
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u)
-            if (sh.v0 + at + u * NT < sh.v1) {
-                const uint32_t bits = mark[at + u * NT + 1];
-                if (bits) Elem<T>::mask(now[u], bits);
-            }
-        run.batch(now, p.c);
+                   for (int u = 0; u < kBatch; ++u) any |= bits[u] = decltype(whole)::value || u < have ? mark[at + u * NT] : 0;
+                   if (any) {
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) now[u] = next[u];
-    }
+                       for (int u = 0; u < kBatch; ++u) Elem<T>::mask(v[u], bits[u]);
+                   }
+                   run.template batch<decltype(whole)::value>(v, have, p.c);
+               });
     if (sh.single >= 0) {
         constexpr int E = Elem<T>::E;
         const int at = sh.single - (sh.head + sh.v0 * E) + E;
         if (!((mark[at / E] >> (at % E)) & 1)) run.one(Elem<T>::get(sh.row + sh.single), p.c);
     }
-    Stats st;
-    run.sums(st.s, st.t);
-    st.m = run.m;
-    st.bad = run.bad ? 1 : 0;
-    st = join_row<NT>(st, warps, &mine, p.ctas, p.c);
+    const Stats st = join_row<NT>(run, part, &mine, p.ctas, p.c);
     if (rank == 0 && tid < 32) {
         finish_row(p, &te, st, 0.0f);
         __syncwarp();
@@ -798,7 +887,7 @@ __global__ void __launch_bounds__(kGradThreads)
 distill_grad_kernel(const T* logits, T* grad, int marks_at, const DistillParams p) {
     constexpr int NT = kGradThreads, E = Elem<T>::E;
     extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ Stats warps[NT / 32];
+    __shared__ Stats part[NT / 32];
     __shared__ Stats mine;
     __shared__ Teacher te;
     uint32_t* marks = reinterpret_cast<uint32_t*>(smem + marks_at);
@@ -846,26 +935,23 @@ distill_grad_kernel(const T* logits, T* grad, int marks_at, const DistillParams 
                     if (bits) Elem<T>::mask(now[u], bits);
                 }
             }
-            run.batch(now, p.c);
+            run.template batch<false>(now, min((g + 1) * group, (nv - tid + NT - 1) / NT) - i, p.c);
         }
     }
     if (sh.single >= 0) {
         const int at = sh.single - origin;
         if (!((mark[at / E] >> (at % E)) & 1)) run.one(Elem<T>::get(sh.row + sh.single), p.c);
     }
-    Stats st;
-    run.sums(st.s, st.t);
-    st.m = run.m;
-    st.bad = run.bad ? 1 : 0;
-    st = join_row<NT>(st, warps, &mine, p.ctas, p.c);  // (its barriers also make the whole share visible to all threads)
+    const Stats st = join_row<NT>(run, part, &mine, p.ctas, p.c);  // (its barriers also make the whole share visible to all threads)
     if (tid < 32) finish_row(p, &te, st, w);
     __syncthreads();
     // a row that counts nothing has no gradient, whatever its logits hold; one without a distribution has NaN
     const bool zero = w == 0.0f, none = !zero && te.none;
     const float f = zero ? 0.0f : none ? quiet_nan() : te.scale_rest, f_own = none ? quiet_nan() : te.scale_own;
-    const float m_rest = te.m_rest;
+    const float m_rest = te.m_rest, nb = -__fmul_rn(m_rest, p.c);
+    const bool far = fabsf(m_rest) > kFar;
     auto value = [&](float x) {  // (of the teacher's tokens, whose exponent may overflow, it is overwritten)
-        const float e = ex2((x - m_rest) * p.c) * f;
+        const float e = ex2(far ? (x - m_rest) * p.c : fmaf(x, p.c, nb)) * f;
         return zero ? 0.0f : e;
     };
     T* out = grad + (long long)row * p.ldd;
@@ -920,7 +1006,7 @@ distill_grad_kernel(const T* logits, T* grad, int marks_at, const DistillParams 
         if (te.repeated)
             for (int i = tid + 1; i < p.k; ++i)
                 if (te.index[i] == te.index[tid]) sum += te.p[i];
-        const float q = ex2((te.x[tid] - te.m) * p.c) * f_own;
+        const float q = ex2(rel(te.x[tid], te.m, p.c)) * f_own;
         out[te.index[tid]] = from_float<T>(zero ? 0.0f : q - (float)(sum * masses(p, &te).keep) * (w * p.inv_t));
     }
     // the loss, while the other warps are done or still write
