@@ -266,7 +266,7 @@ bcq_status bcq_alpha_unpack(long long count, int nseg, const long long* seg_begi
  *
  * The other 4-bit form of a matrix: what the tensor core multiplies as it is (the OCP microscaling format MXFP4).  Blocks of 32
  * consecutive elements of a row share a power of two, the last block of a row may be shorter; an element is a sign and one of
- * 0, 1/2, 1, 3/2, 2, 3, 4, 6 times it.  A matrix of `rows` x `cols` (cols <= 2^20) is held in two buffers, both 16-byte aligned:
+ * 0, 1/2, 1, 3/2, 2, 3, 4, 6 times it.  A matrix of `rows` x `cols` (at most 2^30 and 2^20) is held in two buffers, both 16-byte aligned:
  *   codes  : uint8 [rows][64 * ceil(cols / 128)], element k of a row in byte k / 2, even k in the low half; bit 3 is the sign, bits
  *            0 - 2 number the magnitudes above.  Elements behind a row's last are 0.
  *   scales : uint8 [ceil(rows / 128)][ceil(cols / 128)][32][4][4], exponent + 127 of row r and block b at
@@ -293,7 +293,7 @@ bcq_status bcq_mx_linear(int d_out, int d_in, int n, const uint8_t* x_codes, con
 /* ------------------------------------------------------------------ logits: answers and losses
  *
  * Operators over n rows of `vocab` logits, dtype BCQ_F32 or BCQ_BF16, row pitch ld >= vocab elements.  Rows may start at
- * any element (no alignment beyond that of an element).  n = 0 is allowed and launches nothing; vocab <= 393216 and
+ * any element (no alignment beyond that of an element).  n = 0 is allowed and launches nothing; n <= 2^30, vocab <= 393216 and
  * lists of up to 128 tokens are covered (BCQ_ERR_UNSUPPORTED otherwise); 1e-3 <= temperature <= 1e3 (BCQ_ERR_SHAPE).
  * Logits of -inf are tokens that cannot occur.  A row that has a NaN or +inf, or nothing above -inf, is no
  * distribution: its results are NaN (indices -1).  Sums are kept in fp32 relative to the row's maximum and joined in a

@@ -18,6 +18,7 @@ using namespace bcq;
 __device__ int g_timeout_flag = 0;
 
 constexpr int kMxMaxCols = 1 << 20;
+constexpr int kMxMaxRows = 1 << 30;
 
 inline size_t mx_pitch(int cols) { return (size_t)64 * (((size_t)cols + 127) / 128); }
 inline int mx_atoms(int cols) { return ceil_div(cols, 128); }
@@ -428,7 +429,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
             }
             ptx::tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(acc_empty + 8 * acc) : "memory");
+            if (lane == 0) ptx::mbar_arrive(acc_empty + 8 * acc);
             if (!works) continue;
             if (p.splits > 1) {
 #pragma unroll
@@ -535,7 +536,7 @@ bcq_status launch_mx(const CUtensorMap& tw, const CUtensorMap& tx, const MxLinea
 
 bcq_status check_mx(int rows, int cols, const void* codes, const void* scales) {
     if (rows < 0 || cols < 1) return BCQ_ERR_SHAPE;
-    if (cols > kMxMaxCols) return BCQ_ERR_UNSUPPORTED;
+    if (cols > kMxMaxCols || rows > kMxMaxRows) return BCQ_ERR_UNSUPPORTED;
     if (rows == 0) return BCQ_OK;
     if (!codes || !scales) return BCQ_ERR_NULL;
     if (!aligned16(codes) || !aligned16(scales)) return BCQ_ERR_ALIGN;

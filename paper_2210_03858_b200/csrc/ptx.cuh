@@ -48,6 +48,10 @@ __device__ __forceinline__ void mbar_arrive_expect_tx(uint32_t bar, uint32_t byt
                  : "memory");
 }
 
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
 // One try: the hardware may park the thread for up to `suspend_ns` while the phase is pending and
 // wakes it when the phase completes, so a waiting warp does not burn issue slots or shared-memory
 // bandwidth.  Returns whether the phase with the given parity has completed.

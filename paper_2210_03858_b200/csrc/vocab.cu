@@ -30,6 +30,7 @@ namespace {
 using namespace bcq;
 
 constexpr int kVocabMax = 393216;
+constexpr int kRowsMax = 1 << 30;
 constexpr int kTopMax = 128;
 constexpr int kBatch = 4;          // 16-byte vectors of a thread between two looks at the running maximum
 constexpr float kFloor = -1000.0f; // exponents below are as good as this one (2^-1000 = 0), and 0 * -1000 is 0
@@ -65,6 +66,11 @@ __device__ __forceinline__ void unpack2(f32x2 v, float& a, float& b) { asm("mov.
 __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
     f32x2 r;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
@@ -167,14 +173,15 @@ struct Share {
     int single;        // this thread's
     int first, last;   // elements [first, last) of this CTA
 
-    __device__ __forceinline__ Share(const T* row_, int vocab, int rank, int ctas) : row(row_) {
+    // 2^lg CTAs
+    __device__ __forceinline__ Share(const T* row_, int vocab, int rank, int lg) : row(row_) {
         constexpr int E = Elem<T>::E;
         head = min(vocab, (int)(((16u - (uint32_t)(reinterpret_cast<uintptr_t>(row_) & 15u)) & 15u) / sizeof(T)));
         nvec = (vocab - head) / E;
-        const int per = (nvec + ctas - 1) / ctas;
+        const int ctas = 1 << lg, per = (nvec + ctas - 1) >> lg;
         v0 = min(nvec, rank * per);
         v1 = min(nvec, v0 + per);
-        const int tail0 = head + nvec * E, tid = (int)threadIdx.x;
+        const int tail0 = head + nvec * E, tid = (int)threadIdx.x;  // (a helper warp's threads come last and get none)
         single = -1;
         if (rank == 0 && tid < head) single = tid;
         if (rank == ctas - 1 && tid >= E && tid < E + (vocab - tail0)) single = tail0 + tid - E;  // (head < E)
@@ -264,7 +271,7 @@ struct Running {
 
 // Goes through the vectors of a share, kBatch of a thread at a time, each batch on its way while the one before it is used:
 // use(whole, b, v, have) gets batch b, of which this thread has the first `have` vectors.  The last, incomplete batch
-// comes first: the loop has whole ones only, without a condition on any load.
+// comes first: the loop has whole ones only, without a condition on any load.  start() sends for the first two.
 template <typename T, int NT>
 struct Stream {
     const uint4* at;
@@ -291,12 +298,12 @@ struct Stream {
             if (u < rest) v[u] = ld_stream(at + whole * (kBatch * NT) + u * NT);
         }
     }
-    template <typename Before, typename Use>
-    __device__ __forceinline__ void run(Before before, Use use) const {
-        uint4 a[kBatch], b[kBatch];
+    __device__ __forceinline__ void start(uint4 (&a)[kBatch], uint4 (&b)[kBatch]) const {
         if (more) load_rest(a);
         if (whole > 0) load(0, b);
-        before();
+    }
+    template <typename Use>
+    __device__ __forceinline__ void run(uint4 (&a)[kBatch], uint4 (&b)[kBatch], Use use) const {
         if (more) use(std::false_type(), whole, a, rest);
         for (int i = 0; i < whole; i += 2) {
             if (i + 1 < whole) load(i + 1, a);
@@ -336,6 +343,26 @@ __device__ __forceinline__ unsigned long long key_of(float x, int index) {
     return ((unsigned long long)order_of(x) << 32) | (uint32_t)~index;
 }
 
+// Barrier of the NT threads that go through a row (a helper warp is not among them), and an or over them.
+constexpr uint32_t kRowBarrier = 1;
+template <int NT>
+__device__ __forceinline__ void row_sync() { ptx::named_bar_sync(kRowBarrier, NT); }
+template <int NT>
+__device__ __forceinline__ bool row_sync_or(bool v) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "barrier.cta.red.or.pred q, %2, %3, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t"
+        "}\n"
+        : "=r"(r)
+        : "r"((uint32_t)v), "r"(kRowBarrier), "n"(NT)
+        : "memory");
+    return r != 0;
+}
+
 // Everything of the row, in every thread of the cluster.  `part` holds NT / 32 entries; `mine` is read by the other CTAs.
 // First the maximum, then every thread's sums relative to it.
 template <int NT, typename R>
@@ -346,7 +373,7 @@ __device__ __forceinline__ Stats join_row(const R& run, Stats* part, Stats* mine
     const uint32_t top = __reduce_max_sync(0xffffffffu, order_of(run.m));
     if (lane == 0) part[warp].m = value_of(top);
     Stats v;
-    v.bad = __syncthreads_or(run.bad);
+    v.bad = row_sync_or<NT>(run.bad);
     v.m = value_of(__reduce_max_sync(0xffffffffu, order_of(part[lane & (NW - 1)].m)));
     const float d = fmaxf(rel_base(run.m, v.m == neg_inf() ? 0.0f : v.m, c), kFloor), f = ex2(d);
     v.s = run.s[0] + run.s[1];
@@ -361,7 +388,7 @@ __device__ __forceinline__ Stats join_row(const R& run, Stats* part, Stats* mine
         part[warp].s = v.s;
         part[warp].t = v.t;
     }
-    __syncthreads();
+    row_sync<NT>();
     v.s = part[lane & (NW - 1)].s;
     v.t = part[lane & (NW - 1)].t;
 #pragma unroll
@@ -537,7 +564,7 @@ __device__ __forceinline__ void top_of_share(const Share<T>& sh, int k, float mi
 }
 
 struct LogprobParams {
-    int vocab, ctas, top;
+    int vocab, ctas, lg, top;  // ctas = 2^lg
     long long ld;
     const long long* targets;
     float c, inv_t;
@@ -560,7 +587,7 @@ token_logprobs_kernel(const T* logits, const LogprobParams p) {
     __shared__ Stats mine;
     pdl_wait();
     const int row = (int)blockIdx.x / p.ctas, rank = (int)blockIdx.x % p.ctas;
-    const Share<T> sh(logits + (long long)row * p.ld, p.vocab, rank, p.ctas);
+    const Share<T> sh(logits + (long long)row * p.ld, p.vocab, rank, p.lg);
     const int tid = (int)threadIdx.x;
     TopShared* ts = reinterpret_cast<TopShared*>(smem);
     float* batch_max = reinterpret_cast<float*>(smem + sizeof(TopShared));
@@ -576,11 +603,12 @@ token_logprobs_kernel(const T* logits, const LogprobParams p) {
 
     Running<T, true> run;
     const Stream<T, NT> stream(sh);
-    stream.run([] {},
-               [&](auto whole, int b, uint4(&v)[kBatch], int have) {
-                   const float x = run.template batch<decltype(whole)::value>(v, have, p.c);
-                   if (TOP) batch_max[b * NT + tid] = x;
-               });
+    uint4 va[kBatch], vb[kBatch];
+    stream.start(va, vb);
+    stream.run(va, vb, [&](auto whole, int b, uint4(&v)[kBatch], int have) {
+        const float x = run.template batch<decltype(whole)::value>(v, have, p.c);
+        if (TOP) batch_max[b * NT + tid] = x;
+    });
     if (sh.single >= 0) run.one(single, p.c);
 
     const Stats st = join_row<NT>(run, part, &mine, p.ctas, p.c);
@@ -667,25 +695,29 @@ token_logprobs_kernel(const T* logits, const LogprobParams p) {
 
 // ---------------------------------------------------------------- distillation
 
-// The teacher's tokens of a row.
+// The teacher's tokens of a row, and what a row comes to.
 struct Teacher {
     int index[kTopMax];   // -1: left out
     float logp[kTopMax];
     float x[kTopMax];     // the student's logit of the token
     double p[kTopMax];
-    int first[kTopMax];   // 1: the first entry with this index
-    int repeated;         // some index is there twice
+    int word[kTopMax];       // of its mark; -1: not in this CTA's share
+    float mass_of[kTopMax];  // p of all entries with this index, normalised without a tail; in the first of them
+    int first[kTopMax];      // 1: the first entry with this index
+    double total;            // of p
+    float own_m, own_s;      // largest logit of these tokens, and their sum relative to it
+    float mass, r;           // of the teacher's tokens (1 without a tail), of all others
+    float w;                 // what the row counts
     int bad;
-    double total;         // of p
     // from the whole row
-    int none;             // no distribution
-    float m, s;           // the largest logit, the sum over all tokens
-    float m_rest, s_rest; // the same of the tokens that the teacher does not name (0 and 0: there is none)
-    float scale_rest, scale_own;  // of 2^(c (x - m_rest)) and 2^(c (x - m)) in the gradient
+    int none;                // no distribution
+    float m, s;              // the largest logit, the sum over all tokens
+    float m_rest, s_rest;    // the same of the tokens that the teacher does not name (0 and 0: there is none)
 };
 
 struct DistillParams {
-    int vocab, ctas, k, tail;
+    int n, vocab, ctas, lg, k, tail;  // ctas = 2^lg
+    int marks_bytes;
     long long ld, ldd;
     const int* index;
     const float* logp;
@@ -701,56 +733,104 @@ __device__ __forceinline__ double warp_sum(double v) {
     return v;
 }
 
-// Loads the teacher's list and marks its tokens among this CTA's vectors: bit i of marks[v - v0 + 1] is element i of vector v, the
-// bytes at both ends stand for the single elements before and after the vectors.
-template <typename T, int NT>
-__device__ __forceinline__ void load_teacher(const Share<T>& sh, const DistillParams& p, int row, Teacher* te, uint32_t* marks) {
+// Where element j has its bit in the marks: bit i of byte v - v0 + 1 is element i of vector v, the bytes at both ends stand for the
+// single elements before and after the vectors.
+template <typename T>
+__device__ __forceinline__ int mark_place(const Share<T>& sh, int j) { return j - (sh.head + sh.v0 * Elem<T>::E) + Elem<T>::E; }
+
+// Loads the teacher's list of a row, marks its tokens among this CTA's vectors, and works out what does not need the row's sums.
+// One warp, ahead of those that go through the row.  te and marks are of the row before the last (`used`).
+template <typename T>
+__device__ __forceinline__ void prepare_row(const DistillParams& p, const Share<T>& sh, int row, Teacher* te, uint32_t* marks, bool used) {
     constexpr int E = Elem<T>::E;
-    const int tid = (int)threadIdx.x;
-    int index = -1;
-    float lp = 0.0f;
-    bool bad = false;
-    if (tid < p.k) {
-        index = ld(p.index + (long long)row * p.k + tid);
-        lp = ld(p.logp + (long long)row * p.k + tid);
-        if (index >= p.vocab) bad = true;
-        if (index < 0 || bad) index = -1;
-    }
-    const int words = (sh.v1 - sh.v0 + 2 + 3) / 4;
-    for (int i = tid; i < words; i += NT) marks[i] = 0;
-    if (tid == 0) {
-        te->repeated = p.ctas > 1;  // (a CTA sees repetitions among its own elements only)
-        te->bad = 0;
-    }
-    __syncthreads();
-    if (tid < p.k) {
-        te->index[tid] = index;
-        te->logp[tid] = lp;
-        te->first[tid] = index >= 0;
-        te->p[tid] = index >= 0 ? exp((double)lp) : 0.0;
-        const float x = index >= 0 ? Elem<T>::get(sh.row + index) : neg_inf();
-        te->x[tid] = x;
-        if (bad || !(x < __int_as_float(0x7f800000))) te->bad = 1;
-        if (index >= sh.first && index < sh.last) {
-            const int at = index - (sh.head + sh.v0 * E) + E;  // >= 0: the elements before the first vector are fewer than E
-            const int byte = at / E;
-            const uint32_t bit = 1u << (8 * (byte & 3) + at % E);
-            if (atomicOr(&marks[byte >> 2], bit) & bit) te->repeated = 1;
+    const int lane = (int)threadIdx.x & 31;
+    if (used)
+        for (int i = lane; i < p.k; i += 32)
+            if (te->word[i] >= 0) marks[te->word[i]] = 0;
+    __syncwarp();
+    bool bad = false, again = false;
+    int index[kTopMax / 32];
+    float logp[kTopMax / 32];
+#pragma unroll
+    for (int u = 0; u < kTopMax / 32; ++u) {
+        const int i = u * 32 + lane;
+        index[u] = -1;
+        logp[u] = 0.0f;
+        if (i < p.k) {
+            index[u] = ld(p.index + (long long)row * p.k + i);
+            logp[u] = ld(p.logp + (long long)row * p.k + i);
         }
     }
-    __syncthreads();
-    if (te->repeated && tid < p.k && index >= 0) {
-        bool seen = false;
-        for (int i = 0; i < tid; ++i) seen |= te->index[i] == index;
-        te->first[tid] = !seen;
+    const float w = p.dloss != nullptr ? ld(p.dloss + row) : 0.0f;
+    float x[kTopMax / 32];
+#pragma unroll
+    for (int u = 0; u < kTopMax / 32; ++u) {
+        if (index[u] >= p.vocab) {
+            bad = true;
+            index[u] = -1;
+        }
+        index[u] = max(index[u], -1);
+        x[u] = index[u] >= 0 ? Elem<T>::get(sh.row + index[u]) : neg_inf();
     }
-    if (tid >= 32 && tid < 64) {
-        double total = 0.0;
-        for (int i = tid - 32; i < p.k; i += 32) total += te->p[i];
-        total = warp_sum(total);
-        if (tid == 32) te->total = total;
+    double total = 0.0;
+#pragma unroll
+    for (int u = 0; u < kTopMax / 32; ++u) {
+        const int i = u * 32 + lane;
+        if (i >= p.k) break;
+        te->index[i] = index[u];
+        te->logp[i] = logp[u];
+        te->x[i] = x[u];
+        const double q = index[u] >= 0 ? exp((double)logp[u]) : 0.0;
+        te->p[i] = q;
+        total += q;
+        if (!(x[u] < __int_as_float(0x7f800000))) bad = true;
+        int word = -1;
+        if (index[u] >= sh.first && index[u] < sh.last) {
+            const int at = mark_place(sh, index[u]);  // >= 0: the elements before the first vector are fewer than E
+            const uint32_t bit = 1u << (8 * ((at / E) & 3) + at % E);
+            word = at / E >> 2;
+            if (atomicOr(&marks[word], bit) & bit) again = true;
+        }
+        te->word[i] = word;
     }
-    // (first and total are read after the barriers of join_row)
+    total = warp_sum(total);
+    // an index that is there twice (of several CTAs each sees only its own share)
+    const bool repeated = __any_sync(0xffffffffu, again) || p.ctas > 1;
+    const double keep = p.tail ? 1.0 : (total > 0.0 ? 1.0 / total : 0.0);
+    __syncwarp();
+    float m = neg_inf();
+    for (int i = lane; i < p.k; i += 32) {
+        const int j = te->index[i];
+        bool first = j >= 0;
+        double sum = te->p[i];
+        if (repeated && first) {
+            for (int o = 0; o < i; ++o) first &= te->index[o] != j;
+            for (int o = i + 1; o < p.k; ++o)
+                if (te->index[o] == j) sum += te->p[o];
+        }
+        te->first[i] = first;
+        te->mass_of[i] = (float)(sum * keep);
+        if (first) m = fmaxf(m, te->x[i]);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float s = 0.0f;
+    for (int i = lane; i < p.k; i += 32)
+        if (te->first[i] && m > neg_inf()) s += ex2(fmaxf(rel(te->x[i], m, p.c), kFloor));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    bad = __any_sync(0xffffffffu, bad);
+    if (lane == 0) {
+        te->total = total;
+        te->own_m = m;
+        te->own_s = s;
+        const double mass = p.tail ? total : (total == 0.0 ? 0.0 : total * keep);
+        te->mass = (float)mass;
+        te->r = p.tail ? (float)fmax(0.0, 1.0 - mass) : 0.0f;
+        te->w = w;
+        te->bad = bad;
+    }
+    __syncwarp();
 }
 
 // What a class adds to the divergence, p (d + expm1(-d)) with d = log p - log q: never negative, so near distributions lose
@@ -762,115 +842,37 @@ __device__ __forceinline__ double class_loss(double p, double log_p, double log_
     return p * (d + expm1(-d));
 }
 
-// What P, r and rho are: p sums up to `keep` without a tail.
-struct Masses {
-    double keep, mass, r;
-};
-__device__ __forceinline__ Masses masses(const DistillParams& p, const Teacher* te) {
-    Masses v;
-    const double total = te->total;
-    v.keep = p.tail ? 1.0 : (total > 0.0 ? 1.0 / total : 0.0);
-    v.mass = p.tail ? total : (total == 0.0 ? 0.0 : total * v.keep);
-    v.r = p.tail && te->s_rest > 0.0f ? fmax(0.0, 1.0 - v.mass) : 0.0;
-    return v;
+// Logarithms of e^(x / T), and of a sum's e^(a / T), relative to the base of a sum at m.
+__device__ __forceinline__ double log_rel(float x, float m, const DistillParams& p) {
+    if (fabsf(m) > kFar) return ((double)x - (double)m) * p.inv_t64;
+    return ((double)x * (double)p.c - (double)__fmul_rn(m, p.c)) * 0.69314718055994530942;
+}
+__device__ __forceinline__ double log_rel_base(float a, float m, const DistillParams& p) {
+    if (fabsf(a) > kFar || fabsf(m) > kFar) return ((double)a - (double)m) * p.inv_t64;
+    return ((double)__fmul_rn(a, p.c) - (double)__fmul_rn(m, p.c)) * 0.69314718055994530942;
 }
 
-// The row's sums with the teacher's tokens, and the factors of its gradient, from the sum over all other tokens.  One warp.
-__device__ __forceinline__ void finish_row(const DistillParams& p, Teacher* te, const Stats& rest, float w) {
-    const int lane = (int)threadIdx.x & 31;
-    float m = rest.m;
-    for (int i = lane; i < p.k; i += 32)
-        if (te->first[i]) m = fmaxf(m, te->x[i]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (m == neg_inf()) m = 0.0f;
-    float s = 0.0f;
-    for (int i = lane; i < p.k; i += 32)
-        if (te->first[i]) s += ex2(fmaxf(rel(te->x[i], m, p.c), kFloor));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (lane == 0) {
-        // The rest keeps its own maximum: rho may be too small for a float where its logarithm, and the shares of its
-        // tokens in it, are not.
-        const float down = ex2(fmaxf(rel_base(rest.m, m, p.c), kFloor));
-        te->m_rest = rest.m == neg_inf() ? 0.0f : rest.m;
-        te->s_rest = rest.s;
-        te->m = m;
-        te->s = s + rest.s * down;
-        te->none = rest.bad || te->bad || !(te->s > 0.0f);
-        const Masses v = masses(p, te);
-        const float f = w * p.inv_t, mass = (float)(v.mass + v.r);
-        te->scale_own = f * mass / te->s;
-        te->scale_rest = f * (mass * (down / te->s) - (v.r > 0.0 ? (float)v.r / rest.s : 0.0f));
-    }
-}
-
-// Loss of the row.  One warp, after finish_row.
+// Loss of a row whose sums are there.  One warp.
 __device__ __forceinline__ float loss_of_row(const DistillParams& p, const Teacher* te) {
     const int lane = (int)threadIdx.x & 31;
-    const Masses v = masses(p, te);
-    const double log_s = log((double)te->s), log_keep = p.tail || v.mass == 0.0 ? 0.0 : log(v.keep);
+    const double total = te->total;
+    const double keep = p.tail ? 1.0 : (total > 0.0 ? 1.0 / total : 0.0);
+    const double mass = p.tail ? total : (total == 0.0 ? 0.0 : total * keep);
+    const double r = p.tail && te->s_rest > 0.0f ? fmax(0.0, 1.0 - mass) : 0.0;
+    const double log_s = log((double)te->s), log_keep = p.tail || mass == 0.0 ? 0.0 : log(keep);
     double loss = 0.0;
     for (int i = lane; i < p.k; i += 32) {
         if (te->index[i] < 0) continue;
-        const double log_q = ((double)te->x[i] - (double)te->m) * p.inv_t64 - log_s;
-        loss += class_loss(te->p[i] * v.keep, (double)te->logp[i] + log_keep, log_q);
+        const double log_q = log_rel(te->x[i], te->m, p) - log_s;
+        loss += class_loss(te->p[i] * keep, (double)te->logp[i] + log_keep, log_q);
         if (!te->first[i]) loss -= exp(log_q);  // its q counts once
     }
     loss = warp_sum(loss);
-    const double log_rho = ((double)te->m_rest - (double)te->m) * p.inv_t64 + log((double)te->s_rest) - log_s;
-    loss += class_loss(v.r, log(v.r), log_rho) + (v.mass + v.r - 1.0);
-    if (v.mass == 0.0 && v.r == 0.0) loss = 0.0;  // the teacher says nothing
+    const double log_rho = log_rel_base(te->m_rest, te->m, p) + log((double)te->s_rest) - log_s;
+    loss += class_loss(r, log(r), log_rho) + (mass + r - 1.0);
+    if (mass == 0.0 && r == 0.0) loss = 0.0;  // the teacher says nothing
     return te->none ? quiet_nan() : (float)loss;
 }
-
-constexpr int kLossThreads = 256;
-
-template <typename T>
-__global__ void __launch_bounds__(kLossThreads)
-distill_loss_kernel(const T* logits, const DistillParams p) {
-    constexpr int NT = kLossThreads;
-    extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ Stats part[NT / 32];
-    __shared__ Stats mine;
-    __shared__ Teacher te;
-    uint32_t* marks = reinterpret_cast<uint32_t*>(smem);
-    pdl_wait();
-    const int row = (int)blockIdx.x / p.ctas, rank = (int)blockIdx.x % p.ctas;
-    const Share<T> sh(logits + (long long)row * p.ld, p.vocab, rank, p.ctas);
-    const int tid = (int)threadIdx.x;
-    Running<T, false> run;
-    const uint8_t* mark = reinterpret_cast<const uint8_t*>(marks);
-    const Stream<T, NT> stream(sh);
-    stream.run([&] { load_teacher<T, NT>(sh, p, row, &te, marks); },
-               [&](auto whole, int b, uint4(&v)[kBatch], int have) {
-                   const int at = b * (kBatch * NT) + tid + 1;
-                   uint32_t bits[kBatch], any = 0;
-#pragma unroll
-                   for (int u = 0; u < kBatch; ++u) any |= bits[u] = decltype(whole)::value || u < have ? mark[at + u * NT] : 0;
-                   if (any) {
-#pragma unroll
-                       for (int u = 0; u < kBatch; ++u) Elem<T>::mask(v[u], bits[u]);
-                   }
-                   run.template batch<decltype(whole)::value>(v, have, p.c);
-               });
-    if (sh.single >= 0) {
-        constexpr int E = Elem<T>::E;
-        const int at = sh.single - (sh.head + sh.v0 * E) + E;
-        if (!((mark[at / E] >> (at % E)) & 1)) run.one(Elem<T>::get(sh.row + sh.single), p.c);
-    }
-    const Stats st = join_row<NT>(run, part, &mine, p.ctas, p.c);
-    if (rank == 0 && tid < 32) {
-        finish_row(p, &te, st, 0.0f);
-        __syncwarp();
-        const float loss = loss_of_row(p, &te);
-        if (tid == 0) p.loss[row] = loss;
-    }
-    __syncwarp();
-    if (p.ctas > 1) ptx::cluster_sync();
-}
-
-constexpr int kGradThreads = 512;
 
 template <typename T>
 __device__ __forceinline__ T from_float(float x);
@@ -879,150 +881,239 @@ __device__ __forceinline__ float from_float<float>(float x) { return x; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
-// Four groups of a thread's vectors are on their way into shared memory at once; the sums of a group are taken
-// while the later ones arrive.  The row stays there until its sums are known, and its gradient is written from there, so
-// logits are read once.
+// The gradient of a token that the teacher does not name, f 2^(c x - b).  In bf16 the magnitude of f is part of the exponent (its
+// logarithm is off by 2^-24 of itself, some 2^-19 of the result), which saves a product: the sign is left.
 template <typename T>
-__global__ void __launch_bounds__(kGradThreads)
-distill_grad_kernel(const T* logits, T* grad, int marks_at, const DistillParams p) {
-    constexpr int NT = kGradThreads, E = Elem<T>::E;
+struct RestGrad {
+    float c, nb, f;  // bf16: f is 1 or -1
+
+    __device__ __forceinline__ RestGrad() {}
+    __device__ __forceinline__ RestGrad(float f_, float c_, float b) : c(c_), nb(-b), f(f_) {
+        if (sizeof(T) == 2) {
+            nb += log2f(fabsf(f));
+            f = f < 0.0f ? -1.0f : 1.0f;
+        }
+    }
+    __device__ __forceinline__ float operator()(float x) const { return ex2(fmaf(x, c, nb)) * f; }
+    // of a vector
+    __device__ __forceinline__ uint4 operator()(const uint4& x) const {
+        constexpr int E = Elem<T>::E;
+        const f32x2 c2 = pack2(c, c), nb2 = pack2(nb, nb), f2 = pack2(f, f);
+        const uint32_t sign = f < 0.0f ? 0x80008000u : 0u;
+        uint32_t y[4];
+#pragma unroll
+        for (int i = 0; i < E; i += 2) {
+            float a, b;
+            unpack2(fma2(pack2(Elem<T>::at(x, i), Elem<T>::at(x, i + 1)), c2, nb2), a, b);
+            a = ex2(a);
+            b = ex2(b);
+            if constexpr (sizeof(T) == 4) {
+                unpack2(mul2(pack2(a, b), f2), a, b);
+                y[i] = __float_as_uint(a);
+                y[i + 1] = __float_as_uint(b);
+            } else {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+                memcpy(&y[i / 2], &h, 4);
+                y[i / 2] ^= sign;
+            }
+        }
+        return make_uint4(y[0], y[1], y[2], y[3]);
+    }
+};
+
+// The vector that begins `d` elements into a and goes on in b, 0 < d < E.
+template <typename T>
+__device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, int d) {
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    const int half = d * (int)sizeof(T) / 2;  // in half words
+    if (half & 4) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    }
+    if (half & 2) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    }
+    if (half & 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Written once and not read here: it leaves L2 before the logits that are read again.
+__device__ __forceinline__ void st_stream(uint4* p, const uint4& v) {
+    asm volatile("st.global.cs.v4.b32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+// Elements [first, last) of a row.
+template <typename T>
+__device__ __forceinline__ void zero_row(T* out, int first, int last, int tid, int threads) {
+    constexpr int E = Elem<T>::E;
+    const int before = min(last - first, (int)(((16u - (uint32_t)(reinterpret_cast<uintptr_t>(out + first) & 15u)) & 15u) / sizeof(T)));
+    const int from = first + before, count = (last - from) / E, after = from + count * E;
+    for (int v = tid; v < count; v += threads) st_stream(reinterpret_cast<uint4*>(out + from) + v, make_uint4(0u, 0u, 0u, 0u));
+    if (tid < before) out[first + tid] = from_float<T>(0.0f);
+    if (tid < last - after) out[after + tid] = from_float<T>(0.0f);
+}
+
+constexpr int kDistillThreads = 256;  // that go through a row; one more warp helps them
+
+// Loss, and with GRAD the gradient.  Persistent: a CTA (or a cluster of them) goes from row to row.  Eight warps go through the logits:
+// once for the sums, and for the gradient once more, which finds them in L2 (the rows under way are 60 MB at most).  A ninth
+// is a row ahead of them with the teacher's list, whose loads depend on one another, and a row behind with the loss,
+// which is a chain of logarithms in 64 bits; so neither holds up the loads, of which two batches a thread are always on
+// their way.  Barriers: `ready` when a row's list is there, `done` when its sums are and its list is no longer read; each for
+// odd and for even rows.
+template <typename T, bool GRAD>
+__global__ void __launch_bounds__(kDistillThreads + 32, 3)
+distill_kernel(const T* logits, T* grad, const DistillParams p) {
+    constexpr int NT = kDistillThreads, E = Elem<T>::E;
+    constexpr uint32_t kReady = 2, kDone = 4;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ Stats part[NT / 32];
-    __shared__ Stats mine;
-    __shared__ Teacher te;
-    uint32_t* marks = reinterpret_cast<uint32_t*>(smem + marks_at);
+    __shared__ Stats mine[2];
+    __shared__ Teacher teachers[2];
+    const int tid = (int)threadIdx.x, rank = (int)blockIdx.x & (p.ctas - 1);
+    const int step = (int)gridDim.x >> p.lg;
+    uint32_t* marks = reinterpret_cast<uint32_t*>(smem);
+    for (int i = tid; i < p.marks_bytes / 2; i += NT + 32) marks[i] = 0;
+    __syncthreads();
     pdl_wait();
-    const int row = (int)blockIdx.x / p.ctas, rank = (int)blockIdx.x % p.ctas;
-    const Share<T> sh(logits + (long long)row * p.ld, p.vocab, rank, p.ctas);
-    const int tid = (int)threadIdx.x;
-    // element j of the row is kept[j - origin]: the vectors stay vectors, the elements before them end at the first
-    T* kept = reinterpret_cast<T*>(smem);
-    const int origin = sh.head + sh.v0 * E - E;
-    const uint32_t kept_addr = ptx::smem_u32(smem);
-    const int nv = sh.v1 - sh.v0;
-    const int per_thread = (nv + NT - 1) / NT, group = (per_thread + 3) / 4;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        for (int i = g * group; i < (g + 1) * group; ++i) {
-            const int v = i * NT + tid;
-            if (v < nv) ptx::cp_async_16(kept_addr + 16u * (uint32_t)(v + 1), sh.vec(sh.v0 + v));
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-    if (sh.single >= 0) kept[sh.single - origin] = from_float<T>(Elem<T>::get(sh.row + sh.single));
-    const float w = p.dloss != nullptr ? ld(p.dloss + row) : 0.0f;
-    load_teacher<T, NT>(sh, p, row, &te, marks);
-    const uint8_t* mark = reinterpret_cast<const uint8_t*>(marks);
+    auto share = [&](int row) { return Share<T>(logits + (long long)row * p.ld, p.vocab, rank, p.lg); };
+    int row = (int)blockIdx.x >> p.lg;
 
-    Running<T, false> run;
-    const uint4 masked = make_uint4(Elem<T>::kMasked, Elem<T>::kMasked, Elem<T>::kMasked, Elem<T>::kMasked);
-    const uint4* kept_vec = reinterpret_cast<const uint4*>(smem) + 1;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        if (g == 0) asm volatile("cp.async.wait_group 3;" ::: "memory");
-        if (g == 1) asm volatile("cp.async.wait_group 2;" ::: "memory");
-        if (g == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-        if (g == 3) asm volatile("cp.async.wait_group 0;" ::: "memory");
-        for (int i = g * group; i < (g + 1) * group; i += kBatch) {
-            uint4 now[kBatch];
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const int v = (i + u) * NT + tid;
-                now[u] = masked;
-                if (i + u < (g + 1) * group && v < nv) {
-                    now[u] = kept_vec[v];
-                    const uint32_t bits = mark[v + 1];
-                    if (bits) Elem<T>::mask(now[u], bits);
-                }
+    if (tid >= NT) {
+        int it = 0;
+        for (;; row += step, ++it) {
+            if (row < p.n) {
+                prepare_row<T>(p, share(row), row, &teachers[it & 1], marks + (it & 1) * (p.marks_bytes / 4), it >= 2);
+                asm volatile("bar.arrive %0, %1;" ::"r"(kReady + (it & 1)), "n"(NT + 32) : "memory");
             }
-            run.template batch<false>(now, min((g + 1) * group, (nv - tid + NT - 1) / NT) - i, p.c);
-        }
-    }
-    if (sh.single >= 0) {
-        const int at = sh.single - origin;
-        if (!((mark[at / E] >> (at % E)) & 1)) run.one(Elem<T>::get(sh.row + sh.single), p.c);
-    }
-    const Stats st = join_row<NT>(run, part, &mine, p.ctas, p.c);  // (its barriers also make the whole share visible to all threads)
-    if (tid < 32) finish_row(p, &te, st, w);
-    __syncthreads();
-    // a row that counts nothing has no gradient, whatever its logits hold; one without a distribution has NaN
-    const bool zero = w == 0.0f, none = !zero && te.none;
-    const float f = zero ? 0.0f : none ? quiet_nan() : te.scale_rest, f_own = none ? quiet_nan() : te.scale_own;
-    const float m_rest = te.m_rest, nb = -__fmul_rn(m_rest, p.c);
-    const bool far = fabsf(m_rest) > kFar;
-    auto value = [&](float x) {  // (of the teacher's tokens, whose exponent may overflow, it is overwritten)
-        const float e = ex2(far ? (x - m_rest) * p.c : fmaf(x, p.c, nb)) * f;
-        return zero ? 0.0f : e;
-    };
-    T* out = grad + (long long)row * p.ldd;
-    // whole vectors of the result, whose rows need not start like those of the logits
-    const int before = min(sh.last - sh.first, (int)(((16u - (uint32_t)(reinterpret_cast<uintptr_t>(out + sh.first) & 15u)) & 15u) / sizeof(T)));
-    const int nout = (sh.last - sh.first - before) / E;
-    const int start = sh.first + before;  // the element they begin with
-    uint4* out_vec = reinterpret_cast<uint4*>(out + start);
-    const int pos = start - origin;       // and its place in shared memory
-    if (pos % E == 0) {
-        for (int v = tid; v < nout; v += NT) {
-            const uint4 x = reinterpret_cast<const uint4*>(smem)[pos / E + v];
-            uint32_t y[4];
-            if constexpr (E == 4) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = __float_as_uint(value(Elem<T>::at(x, i)));
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const __nv_bfloat162 h = __floats2bfloat162_rn(value(Elem<T>::at(x, 2 * i)), value(Elem<T>::at(x, 2 * i + 1)));
-                    memcpy(&y[i], &h, 4);
+            if (it > 0) {
+                const int last = (it - 1) & 1;
+                ptx::named_bar_sync(kDone + last, NT + 32);
+                if (rank == 0 && p.loss != nullptr) {
+                    const float loss = loss_of_row(p, &teachers[last]);
+                    if (tid == NT) p.loss[row - step] = loss;
                 }
+                __syncwarp();
             }
-            out_vec[v] = make_uint4(y[0], y[1], y[2], y[3]);
+            if (row >= p.n) break;
+            if (p.ctas > 1) ptx::cluster_sync();  // (that of join_row)
         }
-    } else {
-        for (int v = tid; v < nout; v += NT) {
-            uint32_t y[4];
+    } else if (row < p.n) {
+        uint4 va[kBatch], vb[kBatch];
+        Stream<T, NT>(share(row)).start(va, vb);
+        for (int it = 0; row < p.n; row += step, ++it) {
+            const Share<T> sh = share(row);
+            const Stream<T, NT> stream(sh);
+            const float single = sh.single >= 0 ? Elem<T>::get(sh.row + sh.single) : 0.0f;
+            Teacher* te = &teachers[it & 1];
+            const uint8_t* mark = reinterpret_cast<const uint8_t*>(marks) + (it & 1) * p.marks_bytes;
+            ptx::named_bar_sync(kReady + (it & 1), NT + 32);
+            Running<T, false> run;
+            stream.run(va, vb, [&](auto whole, int b, uint4(&v)[kBatch], int have) {
+                const int at = b * (kBatch * NT) + tid + 1;
+                uint32_t bits[kBatch], any = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const T* from = kept + pos + v * E + i * (E / 4);
-                if constexpr (E == 4) {
-                    y[i] = __float_as_uint(value(from[0]));
+                for (int u = 0; u < kBatch; ++u) any |= bits[u] = decltype(whole)::value || u < have ? mark[at + u * NT] : 0;
+                if (any) {
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u)
+                        if (bits[u]) Elem<T>::mask(v[u], bits[u]);
+                }
+                run.template batch<decltype(whole)::value>(v, have, p.c);
+            });
+            if (sh.single >= 0) {
+                const int at = mark_place(sh, sh.single);
+                if (!((mark[at / E] >> (at % E)) & 1)) run.one(single, p.c);
+            }
+            // what comes next is on its way while the sums are joined: the row again, or the next one
+            const int next = row + step;
+            if (GRAD) stream.start(va, vb);
+            else if (next < p.n) Stream<T, NT>(share(next)).start(va, vb);
+            const Stats rest = join_row<NT>(run, part, &mine[it & 1], p.ctas, p.c);
+            const float own_m = te->own_m, m = fmaxf(rest.m, own_m), base = m == neg_inf() ? 0.0f : m;
+            const float down = ex2(fmaxf(rel_base(rest.m, base, p.c), kFloor));
+            const float s = te->own_s * ex2(fmaxf(rel_base(own_m, base, p.c), kFloor)) + rest.s * down;
+            // The rest keeps its own maximum: rho may be too small for a float where its logarithm, and the shares of its
+            // tokens in it, are not.
+            const float m_rest = rest.m == neg_inf() ? 0.0f : rest.m;
+            const bool none = rest.bad || te->bad || !(s > 0.0f);
+            if (tid == 0) {
+                te->m = base;
+                te->s = s;
+                te->m_rest = m_rest;
+                te->s_rest = rest.s;
+                te->none = none;
+            }
+            if (GRAD) {
+                // a row that counts nothing has no gradient, whatever its logits hold; one without a distribution has NaN
+                const float w = te->w;
+                const bool zero = w == 0.0f;
+                const float r = rest.s > 0.0f ? te->r : 0.0f, f = w * p.inv_t, mass = te->mass + r;
+                const float f_rest = none ? quiet_nan() : f * (mass * (down / s) - (r > 0.0f ? r / rest.s : 0.0f));
+                const RestGrad<T> g(f_rest, p.c, __fmul_rn(m_rest, p.c));
+                const bool far = fabsf(m_rest) > kFar;
+                const float f_own = none ? quiet_nan() : f * mass / s;
+                T* out = grad + (long long)row * p.ldd;
+                // (the teacher's tokens, whose exponent may overflow here, are written after the others)
+                if (zero) {
+                    zero_row(out, sh.first, sh.last, tid, NT);
+                } else if (far) {
+                    for (int j = sh.first + tid; j < sh.last; j += NT)
+                        out[j] = from_float<T>(ex2((Elem<T>::get(sh.row + j) - m_rest) * p.c) * f_rest);
+                } else if (((reinterpret_cast<uintptr_t>(out + sh.head) ^ reinterpret_cast<uintptr_t>(sh.row + sh.head)) & 15u) == 0) {
+                    uint4* out_vec = reinterpret_cast<uint4*>(out + sh.head) + sh.v0 + tid;
+                    stream.run(va, vb, [&](auto whole, int b, uint4(&v)[kBatch], int have) {
+#pragma unroll
+                        for (int u = 0; u < kBatch; ++u)
+                            if (decltype(whole)::value || u < have) st_stream(out_vec + b * (kBatch * NT) + u * NT, g(v[u]));
+                    });
+                    if (sh.single >= 0) out[sh.single] = from_float<T>(g(single));
                 } else {
-                    const __nv_bfloat162 h = __floats2bfloat162_rn(value(__bfloat162float(from[0])), value(__bfloat162float(from[1])));
-                    memcpy(&y[i], &h, 4);
+                    // The result's rows start elsewhere than the logits': its whole vectors, each from two of the logits',
+                    // where both are this CTA's; single elements for the rest.
+                    const int from = sh.head + sh.v0 * E;  // of the elements in whole vectors of logits
+                    const int before = (int)(((16u - (uint32_t)(reinterpret_cast<uintptr_t>(out + from) & 15u)) & 15u) / sizeof(T));
+                    const int count = max(0, sh.v1 - sh.v0 - 1);
+                    uint4* out_vec = reinterpret_cast<uint4*>(out + from + before);
+                    for (int v = tid; v < count; v += kBatch * NT) {
+                        const uint4* at = sh.vec(sh.v0 + v);  // (a neighbour's vector is in L1 by then, or on its way)
+#pragma unroll
+                        for (int u = 0; u < kBatch; ++u)
+                            if (v + u * NT < count) {
+                                va[u] = ld(at + u * NT);
+                                vb[u] = ld(at + u * NT + 1);
+                            }
+#pragma unroll
+                        for (int u = 0; u < kBatch; ++u)
+                            if (v + u * NT < count) st_stream(out_vec + v + u * NT, g(shifted<T>(va[u], vb[u], before)));
+                    }
+                    const int lo = count > 0 ? from + before : sh.last, hi = from + before + count * E;
+                    for (int j = sh.first + tid; j < min(lo, sh.last); j += NT) out[j] = from_float<T>(g(Elem<T>::get(sh.row + j)));
+                    for (int j = hi + tid; count > 0 && j < sh.last; j += NT) out[j] = from_float<T>(g(Elem<T>::get(sh.row + j)));
+                }
+                if (next < p.n) Stream<T, NT>(share(next)).start(va, vb);
+                row_sync<NT>();
+                if (tid < p.k && te->first[tid] && te->index[tid] >= sh.first && te->index[tid] < sh.last) {
+                    const float q = ex2(rel(te->x[tid], base, p.c)) * f_own;
+                    out[te->index[tid]] = from_float<T>(zero ? 0.0f : q - te->mass_of[tid] * f);
                 }
             }
-            out_vec[v] = make_uint4(y[0], y[1], y[2], y[3]);
+            asm volatile("bar.arrive %0, %1;" ::"r"(kDone + (it & 1)), "n"(NT + 32) : "memory");
         }
-    }
-    // single elements at both ends
-    const int after = start + nout * E;
-    int at = -1;
-    if (tid < before) at = sh.first + tid;
-    if (tid >= E && tid < E + (sh.last - after)) at = after + tid - E;
-    if (at >= 0) out[at] = from_float<T>(value((float)kept[at - origin]));
-    __syncthreads();
-    // the teacher's tokens, over what the loops above wrote for them
-    if (tid < p.k && te.first[tid] && te.index[tid] >= sh.first && te.index[tid] < sh.last) {
-        double sum = te.p[tid];
-        if (te.repeated)
-            for (int i = tid + 1; i < p.k; ++i)
-                if (te.index[i] == te.index[tid]) sum += te.p[i];
-        const float q = ex2(rel(te.x[tid], te.m, p.c)) * f_own;
-        out[te.index[tid]] = from_float<T>(zero ? 0.0f : q - (float)(sum * masses(p, &te).keep) * (w * p.inv_t));
-    }
-    // the loss, while the other warps are done or still write
-    if (rank == 0 && p.loss != nullptr && tid >= NT - 32) {
-        const float loss = loss_of_row(p, &te);
-        if (tid == NT - 32) p.loss[row] = loss;
     }
     __syncwarp();
-    if (p.ctas > 1) ptx::cluster_sync();
+    if (p.ctas > 1) ptx::cluster_sync();  // nobody's memory goes away while it is read
 }
 
 // ---------------------------------------------------------------- host side
 
 bcq_status check_rows(int n, int vocab, const void* logits, size_t ld, int dtype, float temperature) {
     if (n < 0 || vocab < 1 || ld < (size_t)vocab) return BCQ_ERR_SHAPE;
-    if (vocab > kVocabMax) return BCQ_ERR_UNSUPPORTED;
+    if (vocab > kVocabMax || n > kRowsMax) return BCQ_ERR_UNSUPPORTED;
     if (dtype != BCQ_F32 && dtype != BCQ_BF16) return BCQ_ERR_UNSUPPORTED;
     if (!(temperature >= 1e-3f && temperature <= 1e3f)) return BCQ_ERR_SHAPE;
     if (n > 0 && logits == nullptr) return BCQ_ERR_NULL;
@@ -1039,6 +1130,8 @@ int ctas_for(int n, int vocab, int elem_bytes, int threads, int per_sm) {
     while (ctas < 8 && (long long)n * ctas * 2 <= (long long)sm_count() * per_sm && nvec / (ctas * 2) >= threads) ctas *= 2;
     return ctas;
 }
+
+int log2_of(int ctas) { return ctas == 8 ? 3 : ctas / 2; }
 
 int max_vectors(int vocab, int elem_bytes, int ctas) { return ceil_div(vocab * elem_bytes / 16, ctas); }
 
@@ -1057,32 +1150,17 @@ bcq_status launch_logprobs(int n, const void* logits, LogprobParams p, cudaStrea
     return BCQ_OK;
 }
 
-template <typename T>
-bcq_status launch_loss(int n, const void* logits, const DistillParams& p, cudaStream_t s) {
-    const size_t smem = align_up((size_t)max_vectors(p.vocab, (int)sizeof(T), p.ctas) + 2, 16);
-    const bcq_status st = ensure_dynamic_smem(distill_loss_kernel<T>, smem);
+template <typename T, bool GRAD>
+bcq_status launch_distill(int n, const void* logits, void* grad, DistillParams p, cudaStream_t s) {
+    p.ctas = ctas_for(n, p.vocab, (int)sizeof(T), kDistillThreads, 3);
+    p.lg = log2_of(p.ctas);
+    p.marks_bytes = (int)align_up((size_t)max_vectors(p.vocab, (int)sizeof(T), p.ctas) + 2, 16);
+    const size_t smem = 2 * (size_t)p.marks_bytes;
+    const bcq_status st = ensure_dynamic_smem(distill_kernel<T, GRAD>, smem);
     if (st != BCQ_OK) return st;
-    BCQ_CUDA_TRY(launch_pdl(distill_loss_kernel<T>, dim3((unsigned)(n * p.ctas)), kLossThreads, smem, s, (unsigned)p.ctas,
-                            (const T*)logits, p));
-    return BCQ_OK;
-}
-
-// Shared memory of a CTA of the gradient: its vectors, one more before and after, the marks.
-size_t grad_kept_bytes(int vocab, int elem_bytes, int ctas) { return (size_t)(max_vectors(vocab, elem_bytes, ctas) + 2) * 16; }
-size_t grad_smem_bytes(int vocab, int elem_bytes, int ctas) {
-    return grad_kept_bytes(vocab, elem_bytes, ctas) + align_up((size_t)max_vectors(vocab, elem_bytes, ctas) + 2, 16);
-}
-
-template <typename T>
-bcq_status launch_grad(int n, const void* logits, void* grad, DistillParams p, cudaStream_t s) {
-    p.ctas = ctas_for(n, p.vocab, (int)sizeof(T), kGradThreads, 2);
-    // two CTAs of an SM, so that one reads while the other writes
-    while (p.ctas < 8 && grad_smem_bytes(p.vocab, (int)sizeof(T), p.ctas) > 108 * 1024) p.ctas *= 2;
-    const size_t smem = grad_smem_bytes(p.vocab, (int)sizeof(T), p.ctas);
-    const bcq_status st = ensure_dynamic_smem(distill_grad_kernel<T>, smem);
-    if (st != BCQ_OK) return st;
-    BCQ_CUDA_TRY(launch_pdl(distill_grad_kernel<T>, dim3((unsigned)(n * p.ctas)), kGradThreads, smem, s, (unsigned)p.ctas,
-                            (const T*)logits, (T*)grad, (int)grad_kept_bytes(p.vocab, (int)sizeof(T), p.ctas), p));
+    const int clusters = std::min(n, std::max(1, sm_count() * 3 / p.ctas));
+    BCQ_CUDA_TRY(launch_pdl(distill_kernel<T, GRAD>, dim3((unsigned)(clusters * p.ctas)), kDistillThreads + 32, smem, s, (unsigned)p.ctas,
+                            (const T*)logits, (T*)grad, p));
     return BCQ_OK;
 }
 
@@ -1112,6 +1190,7 @@ extern "C" bcq_status bcq_token_logprobs(int n, int vocab, const void* logits, s
     p.c = exponent_scale(temperature); p.inv_t = 1.0f / temperature;
     p.logprob = logprob; p.entropy = entropy; p.top_logprob = top_logprob; p.top_index = top_index;
     p.ctas = ctas_for(n, vocab, dtype == BCQ_BF16 ? 2 : 4, kLpThreads, 3);
+    p.lg = log2_of(p.ctas);
     cudaStream_t s = (cudaStream_t)stream;
     return dtype == BCQ_BF16 ? launch_logprobs<__nv_bfloat16>(n, logits, p, s) : launch_logprobs<float>(n, logits, p, s);
 }
@@ -1124,13 +1203,13 @@ extern "C" bcq_status bcq_distill_loss(int n, int vocab, int k, const void* logi
     if (n == 0) return BCQ_OK;
     if (!loss) return BCQ_ERR_NULL;
     DistillParams p;
-    p.vocab = vocab; p.k = k; p.tail = tail != 0; p.ld = (long long)ld; p.ldd = 0;
+    p.n = n; p.vocab = vocab; p.k = k; p.tail = tail != 0; p.ld = (long long)ld; p.ldd = 0;
     p.index = top_index; p.logp = top_logprob; p.dloss = nullptr;
     p.c = exponent_scale(temperature); p.inv_t = 1.0f / temperature; p.inv_t64 = 1.0 / (double)temperature;
     p.loss = loss;
-    p.ctas = ctas_for(n, vocab, dtype == BCQ_BF16 ? 2 : 4, kLossThreads, 3);
     cudaStream_t s = (cudaStream_t)stream;
-    return dtype == BCQ_BF16 ? launch_loss<__nv_bfloat16>(n, logits, p, s) : launch_loss<float>(n, logits, p, s);
+    return dtype == BCQ_BF16 ? launch_distill<__nv_bfloat16, false>(n, logits, nullptr, p, s)
+                             : launch_distill<float, false>(n, logits, nullptr, p, s);
 }
 
 extern "C" bcq_status bcq_distill_grad(int n, int vocab, int k, const void* logits, size_t ld, int dtype, const int* top_index,
@@ -1145,10 +1224,10 @@ extern "C" bcq_status bcq_distill_grad(int n, int vocab, int k, const void* logi
     if ((reinterpret_cast<uintptr_t>(dlogits) & (dtype == BCQ_BF16 ? 1u : 3u)) != 0) return BCQ_ERR_ALIGN;
     if (dlogits == logits && lddl != ld) return BCQ_ERR_SHAPE;
     DistillParams p;
-    p.vocab = vocab; p.k = k; p.tail = tail != 0; p.ld = (long long)ld; p.ldd = (long long)lddl;
+    p.n = n; p.vocab = vocab; p.k = k; p.tail = tail != 0; p.ld = (long long)ld; p.ldd = (long long)lddl;
     p.index = top_index; p.logp = top_logprob; p.dloss = dloss;
     p.c = exponent_scale(temperature); p.inv_t = 1.0f / temperature; p.inv_t64 = 1.0 / (double)temperature;
-    p.loss = loss; p.ctas = 1;
+    p.loss = loss;
     cudaStream_t s = (cudaStream_t)stream;
-    return dtype == BCQ_BF16 ? launch_grad<__nv_bfloat16>(n, logits, dlogits, p, s) : launch_grad<float>(n, logits, dlogits, p, s);
+    return dtype == BCQ_BF16 ? launch_distill<__nv_bfloat16, true>(n, logits, dlogits, p, s) : launch_distill<float, true>(n, logits, dlogits, p, s);
 }
