@@ -461,25 +461,40 @@ def alpha_unpack(packed, alpha_flat, segments: Segments):
                                   _ptr(packed), _ptr(alpha_flat), _stream()), "bcq_alpha_unpack")
 
 
-# ---------------------------------------------------------------------------- operands of the calls below
+# ---------------------------------------------------------------------------- calls that take and return tensors
 
-def _device_of(name, t, dtype=None, shape=None):
-    """Checks an operand: on the current device (the stream is that device's), of the type and shape given, dense."""
+_tensor_call = None
+
+
+def _ops():
+    """The native entry points of the calls below (csrc/binding_torch.cpp), bound to the loaded library."""
+    global _tensor_call
+    if _tensor_call is None:
+        _torch()
+        lib()
+        import importlib
+        try:
+            mod = importlib.import_module(__name__ + "._tensor_call")
+        except ImportError as e:
+            raise RuntimeError("binding not built: run paper_2210_03858_b200/build.py (%s)" % e) from e
+        mod.load(LIB_PATH)
+        _tensor_call = mod
+    return _tensor_call
+
+
+def _done(r, what: str):
+    if type(r) is int:  # a status
+        _check(r, what)
+    return r
+
+
+def _is_bf16(dtype) -> bool:
     torch = _torch()
-    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
-        raise ValueError("%s must be on the current CUDA device" % name)
-    if dtype is not None and t.dtype != dtype:
-        raise TypeError("%s must be %s" % (name, dtype))
-    if shape is not None and (tuple(t.shape) != shape or not t.is_contiguous()):
-        raise ValueError("%s must be contiguous, of shape %s" % (name, list(shape)))
-
-
-def _rows(name, t):
-    """(rows, columns, row pitch) of a matrix whose rows are dense."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("%s must have two dimensions and dense rows" % name)
-    n, cols = t.shape
-    return n, cols, t.stride(0) if n > 1 else max(cols, t.stride(0))
+    if dtype is None or dtype is torch.float32:
+        return False
+    if dtype is torch.bfloat16:
+        return True
+    raise TypeError("output must be float32 or bfloat16")
 
 
 # ---------------------------------------------------------------------------- microscaled 4-bit floating point
@@ -488,60 +503,34 @@ class MxMatrix:
     """A matrix in microscaled 4-bit floating point: codes uint8 [rows][64 * ceil(cols / 128)] and scales uint8
     [ceil(rows / 128)][ceil(cols / 128)][32][4][4] (the container of include/bcq.h)."""
 
+    __slots__ = ("codes", "scales", "rows", "cols")
+
     def __init__(self, codes, scales, rows: int, cols: int):
-        torch = _torch()
-        if rows < 0 or cols < 1:
-            raise ValueError("rows must be at least 0, cols at least 1")
-        a = -(-cols // 128)
-        _device_of("codes", codes, torch.uint8, (rows, 64 * a))
-        _device_of("scales", scales, torch.uint8, (-(-rows // 128), a, 32, 4, 4))
+        _ops().mx_check(codes, scales, rows, cols)
         self.codes, self.scales, self.rows, self.cols = codes, scales, rows, cols
 
 
 def mx_quantize(X) -> MxMatrix:
     """bcq_mx_quantize: X fp32 or bf16 [rows][cols] to microscaled 4-bit floating point."""
-    torch = _torch()
-    _device_of("X", X)
-    rows, cols, ld = _rows("X", X)
-    a = -(-cols // 128)
-    codes = _empty(X, (rows, 64 * a), torch.uint8)
-    scales = _empty(X, (-(-rows // 128), a, 32, 4, 4), torch.uint8)
-    _check(_fn().mx_quantize(rows, cols, _ptr(X), ld, _dtype_code(X), _ptr(codes), _ptr(scales), _stream()), "bcq_mx_quantize")
-    return MxMatrix(codes, scales, rows, cols)
+    M = MxMatrix.__new__(MxMatrix)
+    M.codes, M.scales, M.rows, M.cols = _done(_ops().mx_quantize(X), "bcq_mx_quantize")
+    return M
 
 
 def mx_dequantize(M: MxMatrix, out_dtype=None):
     """bcq_mx_dequantize: the values of M, fp32 or (as exactly) bf16."""
-    torch = _torch()
-    _device_of("M", M.codes)
-    out = _empty(M.codes, (M.rows, M.cols), out_dtype or torch.float32)
-    _check(_fn().mx_dequantize(M.rows, M.cols, _ptr(M.codes), _ptr(M.scales), _ptr(out), M.cols, _dtype_code(out), _stream()),
-           "bcq_mx_dequantize")
-    return out
+    return _done(_ops().mx_dequantize(M.codes, M.scales, M.rows, M.cols, _is_bf16(out_dtype)), "bcq_mx_dequantize")
 
 
 def mx_linear(X, W: MxMatrix, bias=None, out=None, out_dtype=None):
     """bcq_mx_linear: X (an MxMatrix [n][d_in], or fp32 or bf16 values that are quantised first) through W [d_out][d_in] -> Y
     [n][d_out], fp32 unless ``out`` or ``out_dtype`` says bf16.  The same call serves one token and a whole prompt."""
-    torch = _torch()
     if not isinstance(X, MxMatrix):
         X = mx_quantize(X)
-    if X.cols != W.cols:
-        raise ValueError("X has %d columns, W %d" % (X.cols, W.cols))
-    _device_of("X", X.codes)
-    _device_of("W", W.codes)
-    n, d_out = X.rows, W.rows
-    if bias is not None:
-        _device_of("bias", bias, torch.float32, (d_out,))
-    if out is None:
-        out = _empty(X.codes, (n, d_out), out_dtype or torch.float32)
-    _device_of("out", out, out_dtype)
-    if tuple(out.shape) != (n, d_out):
-        raise ValueError("out must have shape %s" % [n, d_out])
-    _, _, ldy = _rows("out", out)
-    _check(_fn().mx_linear(d_out, W.cols, n, _ptr(X.codes), _ptr(X.scales), _ptr(W.codes), _ptr(W.scales), _ptr(bias), _ptr(out), ldy,
-                           _dtype_code(out), _stream()), "bcq_mx_linear")
-    return out
+    if out is not None and out_dtype is not None and out.dtype != out_dtype:
+        raise TypeError("out must be %s" % out_dtype)
+    return _done(_ops().mx_linear(X.codes, X.scales, X.rows, X.cols, W.codes, W.scales, W.rows, W.cols, bias, out, _is_bf16(out_dtype)),
+                 "bcq_mx_linear")
 
 
 # ---------------------------------------------------------------------------- logits: answers and losses
@@ -549,65 +538,20 @@ def mx_linear(X, W: MxMatrix, bias=None, out=None, out_dtype=None):
 def token_logprobs(logits, targets=None, top_k: int = 0, temperature: float = 1.0):
     """bcq_token_logprobs: logits bf16 or fp32 [n][vocab], targets int64 [n] or None -> (logprob fp32 [n] or None, entropy
     fp32 [n], top_logprob fp32 [n][top_k], top_index int32 [n][top_k]) of softmax(logits / temperature)."""
-    torch = _torch()
-    _device_of("logits", logits)
-    n, vocab, ld = _rows("logits", logits)
-    dtype = _dtype_code(logits)
-    if targets is not None:
-        _device_of("targets", targets, torch.int64, (n,))
-    k = max(0, top_k)
-    logprob = None if targets is None else _empty(logits, (n,), torch.float32)
-    entropy = _empty(logits, (n,), torch.float32)
-    top, index = _empty(logits, (n, k), torch.float32), _empty(logits, (n, k), torch.int32)
-    _check(_fn().token_logprobs(n, vocab, _ptr(logits), ld, dtype, _ptr(targets), top_k, temperature, _ptr(logprob),
-                                _ptr(entropy), _ptr(top) if k else None, _ptr(index) if k else None, _stream()),
-           "bcq_token_logprobs")
-    return logprob, entropy, top, index
-
-
-def _teacher(n, top_index, top_logprob):
-    torch = _torch()
-    if top_index.dim() != 2:
-        raise ValueError("top_index must have two dimensions")
-    k = top_index.shape[1]
-    _device_of("top_index", top_index, torch.int32, (n, k))
-    _device_of("top_logprob", top_logprob, torch.float32, (n, k))
-    return k
+    return _done(_ops().token_logprobs(logits, targets, top_k, temperature), "bcq_token_logprobs")
 
 
 def distill_loss(logits, top_index, top_logprob, temperature: float = 1.0, tail: bool = True):
     """bcq_distill_loss: student logits bf16 or fp32 [n][vocab], the teacher's top_index int32 and top_logprob fp32 [n][k] (as
     token_logprobs gives them at the same temperature) -> loss fp32 [n]."""
-    torch = _torch()
-    _device_of("logits", logits)
-    n, vocab, ld = _rows("logits", logits)
-    k = _teacher(n, top_index, top_logprob)
-    loss = _empty(logits, (n,), torch.float32)
-    _check(_fn().distill_loss(n, vocab, k, _ptr(logits), ld, _dtype_code(logits), _ptr(top_index), _ptr(top_logprob), temperature,
-                              1 if tail else 0, _ptr(loss), _stream()), "bcq_distill_loss")
-    return loss
+    return _done(_ops().distill_loss(logits, top_index, top_logprob, temperature, tail), "bcq_distill_loss")
 
 
 def distill_grad(logits, top_index, top_logprob, dloss, temperature: float = 1.0, tail: bool = True, out=None):
     """bcq_distill_grad: as distill_loss, with dloss fp32 [n] (what the loss of each row counts) -> (loss fp32 [n], dlogits
     [n][vocab] in the type of the logits).  ``out`` may be the logits themselves.  dlogits created here is a view whose rows are
     16-byte aligned, so a bf16 one is a dY for linear_bwd_x and linear_bwd_alpha."""
-    torch = _torch()
-    _device_of("logits", logits)
-    n, vocab, ld = _rows("logits", logits)
-    k = _teacher(n, top_index, top_logprob)
-    _device_of("dloss", dloss, torch.float32, (n,))
-    dtype = _dtype_code(logits)
-    if out is None:
-        out = _empty(logits, (n, -(-vocab // 8) * 8), logits.dtype)[:, :vocab]
-    _device_of("out", out, logits.dtype)
-    if out.shape != logits.shape:
-        raise ValueError("out must have the shape of the logits")
-    _, _, ldd = _rows("out", out)
-    loss = _empty(logits, (n,), torch.float32)
-    _check(_fn().distill_grad(n, vocab, k, _ptr(logits), ld, dtype, _ptr(top_index), _ptr(top_logprob), temperature, 1 if tail else 0,
-                              _ptr(dloss), _ptr(loss), _ptr(out), ldd, _stream()), "bcq_distill_grad")
-    return loss, out
+    return _done(_ops().distill_grad(logits, top_index, top_logprob, dloss, temperature, tail, out), "bcq_distill_grad")
 
 
 def kernel_launches() -> int:

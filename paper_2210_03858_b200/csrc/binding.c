@@ -22,13 +22,6 @@ typedef int (*quantize_fn)(int, int, int, int, const void*, size_t, int, void*, 
 typedef int (*adamw_fn)(long long, int, const void*, const void*, const void*, void*, const void*, void*, void*, long long, float,
                         float, float, float, float, float, void*);
 typedef float (*lr_fn)(float, long long, long long, long long);
-typedef int (*logprobs_fn)(int, int, const void*, size_t, int, const void*, int, float, void*, void*, void*, void*, void*);
-typedef int (*distill_loss_fn)(int, int, int, const void*, size_t, int, const void*, const void*, float, int, void*, void*);
-typedef int (*distill_grad_fn)(int, int, int, const void*, size_t, int, const void*, const void*, float, int, const void*, void*, void*,
-                               size_t, void*);
-typedef int (*mx_quantize_fn)(int, int, const void*, size_t, int, void*, void*, void*);
-typedef int (*mx_dequantize_fn)(int, int, const void*, const void*, void*, size_t, int, void*);
-typedef int (*mx_linear_fn)(int, int, int, const void*, const void*, const void*, const void*, const void*, void*, size_t, int, void*);
 typedef int (*gather_fn)(long long, int, const void*, const void*, void*, void*, void*);
 
 static fwd_fn f_fwd, f_fwd_prepared, f_decode;
@@ -39,12 +32,6 @@ static quantize_fn f_quantize;
 static adamw_fn f_adamw;
 static gather_fn f_pack, f_unpack;
 static lr_fn f_lr;
-static mx_quantize_fn f_mx_quantize;
-static mx_dequantize_fn f_mx_dequantize;
-static mx_linear_fn f_mx_linear;
-static logprobs_fn f_token_logprobs;
-static distill_loss_fn f_distill_loss;
-static distill_grad_fn f_distill_grad;
 
 static inline long long as_int(PyObject* o) { return o == Py_None ? 0 : PyLong_AsLongLong(o); }
 static inline void* as_ptr(PyObject* o) { return o == Py_None ? NULL : PyLong_AsVoidPtr(o); }
@@ -126,42 +113,6 @@ static PyObject* py_adamw(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     END
 }
 
-static PyObject* py_mx_quantize(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-    BEGIN(8, 0xE4u, 0u)
-    st_ = f_mx_quantize(I(0), I(1), P(2), Z(3), I(4), P(5), P(6), P(7));
-    END
-}
-
-static PyObject* py_mx_dequantize(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-    BEGIN(8, 0x9Cu, 0u)
-    st_ = f_mx_dequantize(I(0), I(1), P(2), P(3), P(4), Z(5), I(6), P(7));
-    END
-}
-
-static PyObject* py_mx_linear(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-    BEGIN(12, 0x9F8u, 0u)
-    st_ = f_mx_linear(I(0), I(1), I(2), P(3), P(4), P(5), P(6), P(7), P(8), Z(9), I(10), P(11));
-    END
-}
-
-static PyObject* py_token_logprobs(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-    BEGIN(13, 0x1F24u, 0x80u)
-    st_ = f_token_logprobs(I(0), I(1), P(2), Z(3), I(4), P(5), I(6), f_[7], P(8), P(9), P(10), P(11), P(12));
-    END
-}
-
-static PyObject* py_distill_loss(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-    BEGIN(12, 0xCC8u, 0x100u)
-    st_ = f_distill_loss(I(0), I(1), I(2), P(3), Z(4), I(5), P(6), P(7), f_[8], I(9), P(10), P(11));
-    END
-}
-
-static PyObject* py_distill_grad(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-    BEGIN(15, 0x5CC8u, 0x100u)
-    st_ = f_distill_grad(I(0), I(1), I(2), P(3), Z(4), I(5), P(6), P(7), f_[8], I(9), P(10), P(11), P(12), Z(13), P(14));
-    END
-}
-
 #define GATHER(name)                                                                             \
     static PyObject* py_##name(PyObject* self, PyObject* const* args, Py_ssize_t n) {            \
         BEGIN(7, 0x7Cu, 0u)                                                                      \
@@ -199,9 +150,7 @@ static PyObject* py_load(PyObject* self, PyObject* path) {
         {"bcq_linear_decode_packed", &f_packed}, {"bcq_linear_bwd_x", &f_bwd_x},
         {"bcq_linear_bwd_x_prepared", &f_bwd_x_prepared}, {"bcq_linear_bwd_alpha", &f_bwd_alpha},
         {"bcq_quantize", &f_quantize}, {"bcq_alpha_adamw", &f_adamw}, {"bcq_alpha_pack", &f_pack},
-        {"bcq_alpha_unpack", &f_unpack}, {"bcq_lr_linear_decay", &f_lr}, {"bcq_token_logprobs", &f_token_logprobs},
-        {"bcq_mx_quantize", &f_mx_quantize}, {"bcq_mx_dequantize", &f_mx_dequantize}, {"bcq_mx_linear", &f_mx_linear},
-        {"bcq_distill_loss", &f_distill_loss}, {"bcq_distill_grad", &f_distill_grad},
+        {"bcq_alpha_unpack", &f_unpack}, {"bcq_lr_linear_decay", &f_lr},
     };
     for (size_t k = 0; k < sizeof(table) / sizeof(table[0]); ++k) {
         void* sym = dlsym(h, table[k].name);
@@ -217,6 +166,6 @@ static PyObject* py_load(PyObject* self, PyObject* path) {
 #define M(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {
     M(fwd), M(fwd_prepared), M(decode), M(packed), M(bwd_x), M(bwd_x_prepared), M(bwd_alpha), M(quantize), M(adamw), M(pack),
-    M(unpack), M(lr_linear_decay), M(mx_quantize), M(mx_dequantize), M(mx_linear), M(token_logprobs), M(distill_loss), M(distill_grad), {"load", py_load, METH_O, NULL}, {NULL, NULL, 0, NULL}};
+    M(unpack), M(lr_linear_decay), {"load", py_load, METH_O, NULL}, {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bcq_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit__bcq_call(void) { return PyModule_Create(&module); }
