@@ -272,16 +272,12 @@ struct MxLinearParams {
     int m_tiles, n_tiles;
     int steps;           // of 256 elements of d_in: ceil(atoms / 2)
     int splits;          // CTAs of a cluster, which share a tile's steps
-    long long pitch;     // bytes of a row of codes
-    const uint8_t* w_codes;
     const uint8_t* w_scales;
     const uint8_t* x_scales;
     const float* bias;
     void* Y;
     long long ldy;
 };
-
-constexpr int kPrefetchSteps = 16;  // of a tile's weights: 256 KB, the share of an SM in what a call streams from memory
 
 // BN tokens by 128 outputs.  A stage holds 256 elements of d_in: 128 bytes of codes a row, two atoms of scales a 128 rows.
 template <int BN>
@@ -290,15 +286,14 @@ struct MxTile {
     static constexpr uint32_t kA = 128 * 128, kB = BN * 128;
     static constexpr uint32_t kScaleA = 1024, kScaleB = 1024 * kRowBlocks;
     static constexpr uint32_t kStage = kA + kB + kScaleA + kScaleB;
-    static constexpr int kPerSm = BN <= 64 ? 2 : 1;                 // CTAs
-    static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 6 : BN == 16 ? 5 : 4;
+    static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 6 : BN == 64 ? 8 : BN == 32 ? 9 : 10;
     static constexpr int kAccs = BN == 256 ? 1 : 2;                 // accumulators: with one, a tile's is taken to registers at once
     static constexpr uint32_t kScaleCol = kAccs * BN;               // columns of the scales: 8 + 8 per row block for each stage
     static constexpr uint32_t kScaleCols = 8 + 8 * kRowBlocks;
     static constexpr uint32_t kUsed = kScaleCol + kStages * kScaleCols;
     static constexpr uint32_t kTmemCols = kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
     static constexpr size_t kSmem = (size_t)kStages * kStage + 1024 + 256;
-    static_assert(kUsed <= 512 && kTmemCols * kPerSm <= 512, "tensor memory");
+    static_assert(kUsed <= 512, "tensor memory");
     static_assert(kSmem <= 232448, "shared memory");
     static_assert((size_t)kStages * kStage >= (size_t)BN * 128 * 4, "a tile of partial sums fits over the stages");
 };
@@ -311,7 +306,7 @@ __device__ __forceinline__ void store_out(Out* p, float v) {
 
 // Warp 0: TMA; warp 1: scales to tensor memory and UMMA; warps 2..9: epilogue.
 template <int BN, typename Out>
-__global__ void __launch_bounds__(kThreads, MxTile<BN>::kPerSm)
+__global__ void __launch_bounds__(kThreads, 1)
 mx_linear_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const MxLinearParams p) {
     using Tile = MxTile<BN>;
     constexpr int S = Tile::kStages;
@@ -363,15 +358,6 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
         ptx::tmem_relinquish();
     }
     ptx::tc_fence_before_sync();
-    // The weights of the first tile come into L2 while the kernel before this one, which makes the codes of the tokens, still runs.
-    // (4096 -> 12288, one token, with that kernel: 13.4 us without, 11.0 with)
-    if (warp >= kWorkerWarp0) {
-        const int m0 = (tile0 % p.m_tiles) * 128, lines = min(steps, kPrefetchSteps) * 128;
-        for (int i = (int)threadIdx.x - kWorkerWarp0 * 32; i < lines; i += kWorkerWarps * 32)
-            if (m0 + (i & 127) < p.d_out) ptx::prefetch_l2(p.w_codes + (m0 + (i & 127)) * p.pitch + (step0 + (i >> 7)) * 128);
-        for (int i = (int)threadIdx.x - kWorkerWarp0 * 32; i < min(2 * steps, p.atoms - 2 * step0) * 4; i += kWorkerWarps * 32)
-            ptx::prefetch_l2(p.w_scales + ((long long)(m0 / 128) * p.atoms + 2 * step0) * 512 + i * 128);
-    }
     __syncthreads();
     ptx::tc_fence_after_sync();
     pdl_wait();
@@ -570,8 +556,10 @@ bcq_status make_tmap_codes(CUtensorMap* m, const void* base, int rows, size_t pi
 }
 
 // Which tile, and how many CTAs share one.  Costs in cycles: a step of 256 elements is bound by shared memory, which
-// takes the step's codes once from memory and once to the tensor core at 128 bytes a cycle; an epilogue that nothing
-// hides; joining the partial sums of a cluster.
+// takes the step's codes once from memory and once to the tensor core at 128 bytes a cycle, and takes 440 at least (16 tokens, weights
+// in L2); an epilogue that nothing hides; joining the partial sums of a cluster.  One CTA an SM: with two, and the clusters
+// that this allows, one token through 4096 -> 12288 took 13.2 us and not 8.5.  Measured, one token, 1, 2, 4, 8 CTAs a tile:
+// 16384 -> 4096 19.1, 13.3, 10.0, 10.5 us; 6400 -> 1600 9.8, 8.6, 7.4, 7.0; 1024 -> 1024 5.3, 6.2, 5.9, 6.1.
 struct MxPlan {
     int bn, splits;
 };
@@ -583,11 +571,11 @@ MxPlan plan_mx(int d_out, int atoms, int n) {
     // (tiles of fewer than 128 tokens only where one holds all: tokens' scales come in 128s)
     for (int bn = n <= 16 ? 16 : n <= 32 ? 32 : n <= 64 ? 64 : 128; bn <= 256; bn *= 2) {
         if (bn > 128 && n <= 128) break;
-        const int tiles = m_tiles * ceil_div(n, bn), slots = sm_count() * (bn <= 64 ? 2 : 1);
-        const double cycles = 2.0 * (128 + bn) * 128 / 128 * (bn <= 64 ? 2 : 1), tail = bn == 256 ? 900 : 400;
+        const int tiles = m_tiles * ceil_div(n, bn), slots = sm_count();
+        const double cycles = std::max(440.0, 2.0 * (128 + bn)), tail = bn == 256 ? 900 : 400;
         for (int s = 1; s <= 8 && s <= steps; ++s) {
             if (s > 1 && tiles * s > slots) break;
-            const double cost = (double)ceil_div(tiles * s, slots) * (ceil_div(steps, s) * cycles + tail) + (s > 1 ? 1200 + 4.0 * bn : 0);
+            const double cost = (double)ceil_div(tiles * s, slots) * (ceil_div(steps, s) * cycles + tail) + (s > 1 ? 1900 + 4.0 * bn : 0);
             if (cost < least) {
                 least = cost;
                 best.bn = bn;
@@ -604,7 +592,7 @@ bcq_status launch_mx(const CUtensorMap& tw, const CUtensorMap& tx, const MxLinea
     const bcq_status st = ensure_dynamic_smem(mx_linear_kernel<BN, Out>, Tile::kSmem);
     if (st != BCQ_OK) return st;
     const int tiles = p.m_tiles * p.n_tiles;
-    const int ctas = p.splits > 1 ? tiles * p.splits : std::min(tiles, sm_count() * Tile::kPerSm);
+    const int ctas = p.splits > 1 ? tiles * p.splits : std::min(tiles, sm_count());
     BCQ_CUDA_TRY(launch_pdl(mx_linear_kernel<BN, Out>, dim3((unsigned)ctas), kThreads, Tile::kSmem, s, (unsigned)p.splits, tw, tx, p));
     return BCQ_OK;
 }
@@ -704,7 +692,7 @@ extern "C" bcq_status bcq_mx_linear(int d_out, int d_in, int n, const uint8_t* x
     if (n == 0) return BCQ_OK;
     MxLinearParams p;
     p.d_out = d_out; p.n = n; p.atoms = mx_atoms(d_in); p.steps = ceil_div(p.atoms, 2);
-    p.pitch = (long long)mx_pitch(d_in); p.w_codes = w_codes; p.w_scales = w_scales; p.x_scales = x_scales; p.bias = bias; p.Y = Y; p.ldy = (long long)ldy;
+    p.w_scales = w_scales; p.x_scales = x_scales; p.bias = bias; p.Y = Y; p.ldy = (long long)ldy;
     const MxPlan plan = plan_mx(d_out, p.atoms, n);
     p.splits = plan.splits;
     p.m_tiles = ceil_div(d_out, 128); p.n_tiles = ceil_div(n, plan.bn);
