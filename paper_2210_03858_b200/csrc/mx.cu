@@ -304,6 +304,30 @@ __device__ __forceinline__ void store_out(Out* p, float v) {
     else *p = __float2bfloat16_rn(v);
 }
 
+// The first `have` of a thread's columns (tokens) of one output.  Four pointers, each on its way to every fourth token: an address is
+// one addition, and no addition waits for the one before it (c * ldy in 64 bits: 21 instructions an output, 12000 cycles for a
+// tile of 128 x 256).
+template <int COLS, typename Out>
+__device__ __forceinline__ void store_columns(Out* first, long long ldy, int have, const uint32_t (&v)[COLS], float bias) {
+    Out* y[4];
+    const long long far = 4 * ldy;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = first + i * ldy;
+    if (have >= COLS) {
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) {
+            store_out(y[c & 3], __uint_as_float(v[c]) + bias);
+            y[c & 3] += far;
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) {
+            if (c < have) store_out(y[c & 3], __uint_as_float(v[c]) + bias);
+            y[c & 3] += far;
+        }
+    }
+}
+
 // Warp 0: TMA; warp 1: scales to tensor memory and UMMA; warps 2..9: epilogue.
 template <int BN, typename Out>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -480,26 +504,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
 #pragma unroll
                 for (int c = 0; c < kCols; ++c) partial[(tl + c) * 128 + jl] = steps > 0 ? __uint_as_float(v[c]) : 0.0f;
             } else if (j_ok) {
-                // four pointers, each on its way to every fourth token: an address is one addition, and no addition waits for the
-                // one before it (c * ldy in 64 bits: 21 instructions an output, 12000 cycles a tile of 128 x 256)
-                Out* y[4];
-                const long long far = 4 * p.ldy;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = Y + (t0 + i) * p.ldy + j;
-                const int have = p.n - t0;
-                if (have >= kCols) {
-#pragma unroll
-                    for (int c = 0; c < kCols; ++c) {
-                        store_out(y[c & 3], __uint_as_float(v[c]) + bias);
-                        y[c & 3] += far;
-                    }
-                } else {
-#pragma unroll
-                    for (int c = 0; c < kCols; ++c) {
-                        if (c < have) store_out(y[c & 3], __uint_as_float(v[c]) + bias);
-                        y[c & 3] += far;
-                    }
-                }
+                store_columns<kCols>(Y + (long long)t0 * p.ldy + j, p.ldy, p.n - t0, v, bias);
             }
         }
     }
@@ -535,6 +540,173 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
     }
 }
 
+// A pair of CTAs on a tile of 256 outputs by 256 tokens: each has the codes of its own 128 outputs and of half of the tokens, so a
+// step takes 32 KiB into shared memory and 32 KiB out of it in the 512 cycles that the tensor core needs, where a CTA alone takes
+// 48 and 48.  Otherwise as above.  All copies are counted on the leader's barriers, the scales' too, which therefore come by tensor
+// map: boxes of 1024 bytes (two atoms) by row blocks.
+constexpr uint32_t kPairCodes = 2 * 128 * 128, kPairScales = 3 * 1024, kPairStage = kPairCodes + kPairScales;
+constexpr int kPairStages = 6;
+constexpr uint32_t kPairScaleCol = 256, kPairScaleCols = 24;
+constexpr size_t kPairSmem = (size_t)kPairStages * kPairStage + 1024 + 256;
+static_assert(kPairScaleCol + kPairStages * kPairScaleCols <= 512 && kPairSmem <= 232448, "tensor memory, shared memory");
+
+template <typename Out>
+__global__ void __launch_bounds__(kThreads, 1)
+mx_linear_pair_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x,
+                      const __grid_constant__ CUtensorMap tmap_ws, const __grid_constant__ CUtensorMap tmap_xs, const MxLinearParams p) {
+    constexpr int S = kPairStages;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* smem_gen = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
+    const uint32_t ctl_base = smem_base + S * kPairStage;
+    uint8_t* ctl_gen = smem_gen + S * kPairStage;
+    const uint32_t scales_base = smem_base + S * kPairCodes;
+
+    Ctl ctl;
+    ctl.full = ctl_base;
+    ctl.aready = 0;
+    ctl.empty = ctl_base + 8 * S;
+    ctl.accum = ctl_base + 16 * S;
+    const uint32_t acc_empty = ctl.accum + 8;
+    ctl.spare = ctl.accum + 16;
+    volatile uint32_t* tmem_holder = reinterpret_cast<volatile uint32_t*>(ctl_gen + 16 * S + 24);
+    ctl.abort_flag = reinterpret_cast<volatile int*>(ctl_gen + 16 * S + 28);
+    ctl.device_flag = &g_timeout_flag;
+
+    const int warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
+    const int rank = (int)ptx::cluster_rank();
+    const int num_tiles = p.m_tiles * p.n_tiles;
+    const int tile0 = (int)blockIdx.x >> 1, tile_step = (int)gridDim.x >> 1;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S; ++s) {
+            ptx::mbar_init(ctl.full + 8 * s, 1);
+            ptx::mbar_init(ctl.empty + 8 * s, 1);
+        }
+        ptx::mbar_init(ctl.accum, 1);
+        ptx::mbar_init(acc_empty, 2 * kWorkerWarps);
+        ptx::mbar_init(ctl.spare, 1);
+        *ctl.abort_flag = 0;
+        ptx::fence_mbar_init();
+        ptx::prefetch_tmap(&tmap_w);
+        ptx::prefetch_tmap(&tmap_x);
+        ptx::prefetch_tmap(&tmap_ws);
+        ptx::prefetch_tmap(&tmap_xs);
+    }
+    __syncwarp();
+    if (warp == 1) {
+        ptx::tmem_alloc_pair(ptx::smem_u32(const_cast<uint32_t*>(tmem_holder)), 512);
+        ptx::tmem_relinquish_pair();
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::cluster_sync();  // the peer's barriers exist
+    ptx::tc_fence_after_sync();
+    pdl_wait();
+    const uint32_t tmem_base = *tmem_holder;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            bool ok = true;
+            int s = 0;
+            uint32_t ph = 0;
+            for (int tile = tile0; tile < num_tiles && ok; tile += tile_step) {
+                const int m0 = tile % p.m_tiles, n0 = tile / p.m_tiles;
+                for (int step = 0; step < p.steps; ++step) {
+                    ok = wait_bar(ctl.empty + 8 * s, ph ^ 1u, ctl, 61);
+                    if (!ok) break;
+                    const uint32_t sa = smem_base + s * kPairCodes, sf = scales_base + s * kPairScales;
+                    const uint32_t bar = ptx::leader_addr(ctl.full + 8 * s);
+                    if (rank == 0) ptx::mbar_arrive_expect_tx(ctl.full + 8 * s, 2 * kPairStage);
+                    ptx::tma_load_2d_pair(sa, &tmap_w, step * 128, m0 * 256 + rank * 128, bar);
+                    ptx::tma_load_2d_pair(sa + kABytes, &tmap_x, step * 128, n0 * 256 + rank * 128, bar);
+                    ptx::tma_load_2d_pair(sf, &tmap_ws, step * 256, m0 * 2 + rank, bar);
+                    ptx::tma_load_2d_pair(sf + 1024, &tmap_xs, step * 256, n0 * 2, bar);
+                    if (++s == S) { s = 0; ph ^= 1u; }
+                }
+            }
+            // giving up: the copies in flight land within microseconds; wait a thousand times as long
+            if (!ok) for (int i = 0; i < 1000; ++i) __nanosleep(2000);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (rank == 0 && ptx::elect_one()) {
+            bool ok = true;
+            int s = 0, lt = 0;
+            uint32_t ph = 0;
+            constexpr uint32_t kHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+            for (int tile = tile0; tile < num_tiles && ok; tile += tile_step, ++lt) {
+                ok = wait_bar(acc_empty, (uint32_t)(lt & 1) ^ 1u, ctl, 62, 32u);
+                if (!ok) break;
+                ptx::tc_fence_after_sync();
+                for (int step = 0; step < p.steps; ++step) {
+                    ok = wait_bar(ctl.full + 8 * s, ph, ctl, 63, 32u);
+                    if (!ok) break;
+                    ptx::tc_fence_after_sync();
+                    const uint32_t sa = smem_base + s * kPairCodes, sf = scales_base + s * kPairScales;
+                    const uint32_t col_a = tmem_base + kPairScaleCol + (uint32_t)s * kPairScaleCols, col_b = col_a + 8;
+                    const int atoms = min(2, p.atoms - 2 * step);
+                    for (int a = 0; a < atoms; ++a) {
+                        ptx::tmem_copy_scales_pair(col_a + 4 * a, sf + 512 * a);
+                        ptx::tmem_copy_scales_pair(col_b + 8 * a, sf + 1024 + 512 * a);
+                        ptx::tmem_copy_scales_pair(col_b + 8 * a + 4, sf + 2048 + 512 * a);
+                    }
+                    const uint32_t a_lo = (sa >> 4) & 0x3FFFu, b_lo = ((sa + kABytes) >> 4) & 0x3FFFu;
+                    for (int a = 0; a < atoms; ++a) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int kk = 2 * a + h;
+                            ptx::umma_mxf4_pair(tmem_base, a_lo + 2 * kk, kHi, b_lo + 2 * kk, kHi,
+                                                h ? ptx::make_idesc_mxf4(256, 256, 1) : ptx::make_idesc_mxf4(256, 256, 0), col_a + 4 * a,
+                                                col_b + 8 * a, (step > 0 || kk > 0) ? 1u : 0u);
+                        }
+                    }
+                    ptx::umma_commit_pair(ctl.empty + 8 * s);
+                    if (++s == S) { s = 0; ph ^= 1u; }
+                }
+                if (ok) ptx::umma_commit_pair(ctl.accum);
+            }
+            if (!ok) {
+                ptx::umma_commit_pair(ctl.spare);
+                wait_bar(ctl.spare, 0, ctl, 64);
+            }
+        }
+        __syncwarp();
+    } else {
+        const int quarter = warp & 3;
+        const int half = (warp - kWorkerWarp0) >> 2;
+        bool ok = true;
+        int lt = 0;
+        for (int tile = tile0; tile < num_tiles && ok; tile += tile_step, ++lt) {
+            const int m0 = tile % p.m_tiles, n0 = tile / p.m_tiles;
+            const int j = m0 * 256 + rank * 128 + quarter * 32 + lane, t0 = n0 * 256 + half * 128;
+            const bool j_ok = j < p.d_out;
+            const float bias = p.bias != nullptr && j_ok ? ld(p.bias + j) : 0.0f;
+            ok = wait_bar(ctl.accum, (uint32_t)lt & 1u, ctl, 65, 64u);
+            if (!ok) break;
+            ptx::tc_fence_after_sync();
+            // the accumulator goes to registers at once, and the next tile's products may begin
+            uint32_t v[128];
+#pragma unroll
+            for (int c = 0; c < 128; c += 32) ptx::tmem_ld_x32(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 128 + c), v + c);
+            ptx::tmem_ld_wait();
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive_cluster(ptx::leader_addr(acc_empty));
+            if (j_ok) store_columns<128>(reinterpret_cast<Out*>(p.Y) + (long long)t0 * p.ldy + j, p.ldy, p.n - t0, v, bias);
+        }
+    }
+
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::cluster_sync();  // neither CTA's memory goes away under the other
+    if (warp == 1) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc_pair(tmem_base, 512);
+    }
+}
+
 // Codes [rows][pitch bytes], boxes of 128 bytes (256 elements) x box_rows, 128-byte swizzle, zeros outside.
 bcq_status make_tmap_codes(CUtensorMap* m, const void* base, int rows, size_t pitch, int box_rows) {
     EncodeTiledFn fn = encode_fn();
@@ -555,6 +727,26 @@ bcq_status make_tmap_codes(CUtensorMap* m, const void* base, int rows, size_t pi
     return BCQ_OK;
 }
 
+// Scales as rows of 32-bit words, one for each 128 rows of the matrix: boxes of two atoms (1024 bytes) by `blocks`, zeros outside.
+bcq_status make_tmap_scales(CUtensorMap* m, const void* base, int rows, int atoms, int blocks) {
+    EncodeTiledFn fn = encode_fn();
+    if (fn == nullptr) {
+        set_last_cuda_error((int)cudaErrorNotSupported);
+        return BCQ_ERR_CUDA;
+    }
+    cuuint64_t dims[2] = {(cuuint64_t)atoms * 128, (cuuint64_t)ceil_div(rows, 128)};
+    cuuint64_t strides[1] = {(cuuint64_t)atoms * 512};
+    cuuint32_t box[2] = {256u, (cuuint32_t)blocks};
+    cuuint32_t estr[2] = {1u, 1u};
+    CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        set_last_cuda_error((int)cudaErrorInvalidValue);
+        return BCQ_ERR_CUDA;
+    }
+    return BCQ_OK;
+}
+
 // Which tile, and how many CTAs share one.  Costs in cycles: a step of 256 elements is bound by shared memory, which
 // takes the step's codes once from memory and once to the tensor core at 128 bytes a cycle, and takes 440 at least (16 tokens, weights
 // in L2); an epilogue that nothing hides; joining the partial sums of a cluster.  One CTA an SM: with two, and the clusters
@@ -562,11 +754,12 @@ bcq_status make_tmap_codes(CUtensorMap* m, const void* base, int rows, size_t pi
 // 16384 -> 4096 19.1, 13.3, 10.0, 10.5 us; 6400 -> 1600 9.8, 8.6, 7.4, 7.0; 1024 -> 1024 5.3, 6.2, 5.9, 6.1.
 struct MxPlan {
     int bn, splits;
+    bool pair;
 };
 
 MxPlan plan_mx(int d_out, int atoms, int n) {
     const int steps = ceil_div(atoms, 2), m_tiles = ceil_div(d_out, 128);
-    MxPlan best = {256, 1};
+    MxPlan best = {256, 1, false};
     double least = 1e30;
     // (tiles of fewer than 128 tokens only where one holds all: tokens' scales come in 128s)
     for (int bn = n <= 16 ? 16 : n <= 32 ? 32 : n <= 64 ? 64 : 128; bn <= 256; bn *= 2) {
@@ -583,7 +776,26 @@ MxPlan plan_mx(int d_out, int atoms, int n) {
             }
         }
     }
+    // a pair on 256 x 256: 512 cycles a step, which the tensor core takes too
+    const double pairs = (double)ceil_div(ceil_div(d_out, 256) * ceil_div(n, 256), std::max(1, sm_count() / 2)) * (steps * 512.0 + 900);
+    if (n > 128 && pairs < least) best.pair = true;
     return best;
+}
+
+template <typename Out>
+bcq_status launch_mx_pair(const uint8_t* x_codes, const uint8_t* w_codes, int d_in, MxLinearParams p, cudaStream_t s) {
+    CUtensorMap tw, tx, tws, txs;
+    bcq_status st;
+    if ((st = make_tmap_codes(&tw, w_codes, p.d_out, mx_pitch(d_in), 128)) != BCQ_OK) return st;
+    if ((st = make_tmap_codes(&tx, x_codes, p.n, mx_pitch(d_in), 128)) != BCQ_OK) return st;
+    if ((st = make_tmap_scales(&tws, p.w_scales, p.d_out, p.atoms, 1)) != BCQ_OK) return st;
+    if ((st = make_tmap_scales(&txs, p.x_scales, p.n, p.atoms, 2)) != BCQ_OK) return st;
+    if ((st = ensure_dynamic_smem(mx_linear_pair_kernel<Out>, kPairSmem)) != BCQ_OK) return st;
+    p.m_tiles = ceil_div(p.d_out, 256);
+    p.n_tiles = ceil_div(p.n, 256);
+    const int pairs = std::min(p.m_tiles * p.n_tiles, std::max(1, sm_count() / 2));
+    BCQ_CUDA_TRY(launch_pdl(mx_linear_pair_kernel<Out>, dim3(2u * (unsigned)pairs), kThreads, kPairSmem, s, 2, tw, tx, tws, txs, p));
+    return BCQ_OK;
 }
 
 template <int BN, typename Out>
@@ -694,6 +906,11 @@ extern "C" bcq_status bcq_mx_linear(int d_out, int d_in, int n, const uint8_t* x
     p.d_out = d_out; p.n = n; p.atoms = mx_atoms(d_in); p.steps = ceil_div(p.atoms, 2);
     p.w_scales = w_scales; p.x_scales = x_scales; p.bias = bias; p.Y = Y; p.ldy = (long long)ldy;
     const MxPlan plan = plan_mx(d_out, p.atoms, n);
+    if (plan.pair) {
+        p.splits = 1;
+        return y_dtype == BCQ_BF16 ? launch_mx_pair<__nv_bfloat16>(x_codes, w_codes, d_in, p, (cudaStream_t)stream)
+                                   : launch_mx_pair<float>(x_codes, w_codes, d_in, p, (cudaStream_t)stream);
+    }
     p.splits = plan.splits;
     p.m_tiles = ceil_div(d_out, 128); p.n_tiles = ceil_div(n, plan.bn);
     CUtensorMap tw, tx;

@@ -299,6 +299,34 @@ __device__ __forceinline__ void umma_mxf4(uint32_t d_tmem, uint32_t a_lo, uint32
         : "memory");
 }
 
+// The same for a pair of CTAs, issued by its leader: the copy takes place in both, each from its own shared memory to its own tensor
+// memory; of A and its scales each CTA has its own 128 rows, of B half of the columns, of B's scales all.
+__device__ __forceinline__ void tmem_copy_scales_pair(uint32_t taddr, uint32_t smem_addr) {
+    const uint32_t lo = (smem_addr >> 4) & 0x3FFFu, hi = (128u >> 4) | (1u << 14);
+    asm volatile(
+        "{\n\t"
+        ".reg .b64 d;\n\t"
+        "mov.b64 d, {%1, %2};\n\t"
+        "tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], d;\n\t"
+        "}\n"
+        ::"r"(taddr), "r"(lo), "r"(hi)
+        : "memory");
+}
+__device__ __forceinline__ void umma_mxf4_pair(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                               uint32_t scale_a, uint32_t scale_b, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        ".reg .b64 da, db;\n\t"
+        "mov.b64 da, {%1, %2};\n\t"
+        "mov.b64 db, {%3, %4};\n\t"
+        "setp.ne.b32 p, %8, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %5, [%6], [%7], p;\n\t"
+        "}\n"
+        ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate)
+        : "memory");
+}
+
 // Instruction descriptor for kind::mxf4, e2m1 inputs (K-major), ue8m0 scales.  A cell of tensor memory holds the scales
 // of 128 elements; `pair` says which two of the four belong to this UMMA (0: the first 64 elements, 1: the second).
 __host__ __device__ constexpr uint32_t make_idesc_mxf4(int M, int N, int pair) {
