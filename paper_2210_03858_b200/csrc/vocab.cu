@@ -417,6 +417,7 @@ struct TopShared {
     unsigned long long cand[kCandidates];
     unsigned long long best[kTopMax];       // of this CTA, in order; 0: none
     unsigned long long others[8 * kTopMax]; // the lists of the cluster
+    int place[kTopMax + 1];                 // in the row's list; the last: how many places are taken
     float largest[kLpThreads];              // of each thread
     int events[kCandidates];
     int num_cand, num_events;
@@ -501,9 +502,20 @@ __device__ __forceinline__ void top_of_share(const Share<T>& sh, int k, float mi
         uint32_t o[NT / 32];
 #pragma unroll
         for (int i = 0; i < NT / 32; ++i) o[i] = order_of(ts->largest[32 * i + tid]);
-        uint32_t lo = 0;  // at least k are as large
+        // (from the first bit on in which the largest and the smallest of them differ)
+        uint32_t most = o[0], least = o[0];
+#pragma unroll
+        for (int i = 1; i < NT / 32; ++i) {
+            most = max(most, o[i]);
+            least = min(least, o[i]);
+        }
+        most = __reduce_max_sync(0xffffffffu, most);
+        least = __reduce_min_sync(0xffffffffu, least);
+        int bit = 31 - __clz((int)(most ^ least));          // -1: all are equal
+        uint32_t lo = bit < 0 ? most : most >> 1 >> bit << bit << 1;  // at least k are as large
+        constexpr int kLast = sizeof(T) == 2 ? 16 : 12;
 #pragma unroll 1
-        for (int bit = 31; bit >= 12; --bit) {
+        for (; bit >= kLast; --bit) {
             const uint32_t mid = lo | (1u << bit);
             int c = 0;
 #pragma unroll
@@ -611,6 +623,8 @@ token_logprobs_kernel(const T* logits, const LogprobParams p) {
     });
     if (sh.single >= 0) run.one(single, p.c);
 
+    // (first, so that the cluster meets once for the sums and the lists; of a row that is no distribution it comes to nothing)
+    if (TOP) top_of_share<T>(sh, p.top, run.m, single, batch_max, stream.batches(), ts);
     const Stats st = join_row<NT>(run, part, &mine, p.ctas, p.c);
     const bool none = st.bad || !(st.s > 0.0f);  // no distribution
     const float log_s = log2f(st.s);
@@ -638,53 +652,35 @@ token_logprobs_kernel(const T* logits, const LogprobParams p) {
                     out_i[i] = -1;
                 }
         } else {
-            top_of_share<T>(sh, k, run.m, single, batch_max, stream.batches(), ts);
             if (p.ctas == 1) {
                 for (int i = tid; i < k; i += NT) put(i, ts->best[i]);
             } else {
-                // each CTA finds the places of its own in the row's list: those of the other lists that come before, by
-                // bisection in copies of them
-                __syncwarp();
-                ptx::cluster_sync();
+                // Each CTA finds the places of its own in the row's list: its place here, and how many of each other list come before
+                // it, by bisection in copies of them.  Rank 0 also counts how many places are taken.
                 for (int i = tid; i < p.ctas * k; i += NT) {
                     unsigned long long key;
                     const uint32_t from = ptx::cluster_addr(ptx::smem_u32(&ts->best[i % k]), (uint32_t)(i / k));
                     asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(key) : "r"(from) : "memory");
                     ts->others[i] = key;
                 }
+                for (int i = tid; i <= k; i += NT) ts->place[i] = 0;
+                __syncthreads();
+                for (int i = tid; i < p.ctas * (k + 1); i += NT) {
+                    const int of = i / p.ctas, r = i % p.ctas;
+                    const unsigned long long* list = ts->others + r * k;
+                    const unsigned long long key = of < k ? ts->best[of] : 0;
+                    int lo = 0, hi = k;  // how many are larger
+                    while (lo < hi) {
+                        const int mid = (lo + hi) >> 1;
+                        if (list[mid] > key) lo = mid + 1;
+                        else hi = mid;
+                    }
+                    atomicAdd(&ts->place[of], lo);
+                }
                 __syncthreads();
                 for (int i = tid; i < k; i += NT) {
-                    const unsigned long long key = ts->best[i];
-                    if (key == 0) continue;
-                    int place = i;
-                    for (int r = 0; r < p.ctas; ++r) {
-                        if (r == rank) continue;
-                        const unsigned long long* list = ts->others + r * k;
-                        int lo = 0, hi = k;  // how many are larger
-                        while (lo < hi) {
-                            const int mid = (lo + hi) >> 1;
-                            if (list[mid] > key) lo = mid + 1;
-                            else hi = mid;
-                        }
-                        place += lo;
-                    }
-                    if (place < k) put(place, key);
-                }
-                // places that no element takes
-                if (rank == 0) {
-                    int have = 0;
-                    for (int r = 0; r < p.ctas; ++r) {
-                        const unsigned long long* list = ts->others + r * k;
-                        int lo = 0, hi = k;
-                        while (lo < hi) {
-                            const int mid = (lo + hi) >> 1;
-                            if (list[mid] != 0) lo = mid + 1;
-                            else hi = mid;
-                        }
-                        have += lo;
-                    }
-                    for (int i = tid; i < k; i += NT)
-                        if (i >= have) put(i, 0);
+                    if (ts->best[i] != 0 && ts->place[i] < k) put(ts->place[i], ts->best[i]);
+                    if (rank == 0 && i >= ts->place[k]) put(i, 0);
                 }
             }
         }
@@ -739,9 +735,10 @@ template <typename T>
 __device__ __forceinline__ int mark_place(const Share<T>& sh, int j) { return j - (sh.head + sh.v0 * Elem<T>::E) + Elem<T>::E; }
 
 // Loads the teacher's list of a row, marks its tokens among this CTA's vectors, and works out what does not need the row's sums.
-// One warp, ahead of those that go through the row.  te and marks are of the row before the last (`used`).
-template <typename T>
-__device__ __forceinline__ void prepare_row(const DistillParams& p, const Share<T>& sh, int row, Teacher* te, uint32_t* marks, bool used) {
+// marked() is called when
+// the marks are there, which are all that the first pass wants.  One warp, ahead of those that go through the row.  te and marks are of the row before the last (`used`).
+template <typename T, typename Marked>
+__device__ __forceinline__ void prepare_row(const DistillParams& p, const Share<T>& sh, int row, Teacher* te, uint32_t* marks, bool used, Marked marked) {
     constexpr int E = Elem<T>::E;
     const int lane = (int)threadIdx.x & 31;
     if (used)
@@ -770,7 +767,33 @@ __device__ __forceinline__ void prepare_row(const DistillParams& p, const Share<
             index[u] = -1;
         }
         index[u] = max(index[u], -1);
-        x[u] = index[u] >= 0 ? Elem<T>::get(sh.row + index[u]) : neg_inf();
+        int word = -1;
+        if (index[u] >= sh.first && index[u] < sh.last) {
+            const int at = mark_place(sh, index[u]);  // >= 0: the elements before the first vector are fewer than E
+            const uint32_t bit = 1u << (8 * ((at / E) & 3) + at % E);
+            word = at / E >> 2;
+            if (atomicOr(&marks[word], bit) & bit) again = true;
+        }
+        if (u * 32 + lane < p.k) te->word[u * 32 + lane] = word;
+    }
+    marked();
+#pragma unroll
+    for (int u = 0; u < kTopMax / 32; ++u) x[u] = index[u] >= 0 ? Elem<T>::get(sh.row + index[u]) : neg_inf();
+    // an index that is there twice: of several CTAs each has marked its own share only, so all are compared
+    if (p.ctas > 1) {
+#pragma unroll
+        for (int u = 0; u < kTopMax / 32; ++u) {
+            if (u * 32 >= p.k) break;
+            const uint32_t same = __match_any_sync(0xffffffffu, index[u] >= 0 ? index[u] : -1 - lane);
+            again |= (same & (same - 1)) != 0;
+#pragma unroll
+            for (int o = 0; o < u; ++o)
+#pragma unroll 4
+                for (int l = 0; l < 32; ++l) {
+                    const int other = __shfl_sync(0xffffffffu, index[o], l);
+                    again |= index[u] >= 0 && other == index[u];
+                }
+        }
     }
     double total = 0.0;
 #pragma unroll
@@ -784,18 +807,9 @@ __device__ __forceinline__ void prepare_row(const DistillParams& p, const Share<
         te->p[i] = q;
         total += q;
         if (!(x[u] < __int_as_float(0x7f800000))) bad = true;
-        int word = -1;
-        if (index[u] >= sh.first && index[u] < sh.last) {
-            const int at = mark_place(sh, index[u]);  // >= 0: the elements before the first vector are fewer than E
-            const uint32_t bit = 1u << (8 * ((at / E) & 3) + at % E);
-            word = at / E >> 2;
-            if (atomicOr(&marks[word], bit) & bit) again = true;
-        }
-        te->word[i] = word;
     }
     total = warp_sum(total);
-    // an index that is there twice (of several CTAs each sees only its own share)
-    const bool repeated = __any_sync(0xffffffffu, again) || p.ctas > 1;
+    const bool repeated = __any_sync(0xffffffffu, again);
     const double keep = p.tail ? 1.0 : (total > 0.0 ? 1.0 / total : 0.0);
     __syncwarp();
     float m = neg_inf();
@@ -963,13 +977,13 @@ constexpr int kDistillThreads = 256;  // that go through a row; one more warp he
 // once for the sums, and for the gradient once more, which finds them in L2 (the rows under way are 60 MB at most).  A ninth
 // is a row ahead of them with the teacher's list, whose loads depend on one another, and a row behind with the loss,
 // which is a chain of logarithms in 64 bits; so neither holds up the loads, of which two batches a thread are always on
-// their way.  Barriers: `ready` when a row's list is there, `done` when its sums are and its list is no longer read; each for
-// odd and for even rows.
+// their way.  Barriers: `ready` when a row's tokens are marked, `listed` when the rest of its list is there, `done` when its sums
+// are and its list is no longer read; each for odd and for even rows.
 template <typename T, bool GRAD>
 __global__ void __launch_bounds__(kDistillThreads + 32, 3)
 distill_kernel(const T* logits, T* grad, const DistillParams p) {
     constexpr int NT = kDistillThreads, E = Elem<T>::E;
-    constexpr uint32_t kReady = 2, kDone = 4;
+    constexpr uint32_t kReady = 2, kListed = 4, kDone = 6;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ Stats part[NT / 32];
     __shared__ Stats mine[2];
@@ -987,8 +1001,11 @@ distill_kernel(const T* logits, T* grad, const DistillParams p) {
         int it = 0;
         for (;; row += step, ++it) {
             if (row < p.n) {
-                prepare_row<T>(p, share(row), row, &teachers[it & 1], marks + (it & 1) * (p.marks_bytes / 4), it >= 2);
-                asm volatile("bar.arrive %0, %1;" ::"r"(kReady + (it & 1)), "n"(NT + 32) : "memory");
+                prepare_row<T>(p, share(row), row, &teachers[it & 1], marks + (it & 1) * (p.marks_bytes / 4), it >= 2, [&] {
+                    __syncwarp();
+                    asm volatile("bar.arrive %0, %1;" ::"r"(kReady + (it & 1)), "n"(NT + 32) : "memory");
+                });
+                asm volatile("bar.arrive %0, %1;" ::"r"(kListed + (it & 1)), "n"(NT + 32) : "memory");
             }
             if (it > 0) {
                 const int last = (it - 1) & 1;
@@ -1034,6 +1051,7 @@ distill_kernel(const T* logits, T* grad, const DistillParams p) {
             if (GRAD) stream.start(va, vb);
             else if (next < p.n) Stream<T, NT>(share(next)).start(va, vb);
             const Stats rest = join_row<NT>(run, part, &mine[it & 1], p.ctas, p.c);
+            ptx::named_bar_sync(kListed + (it & 1), NT + 32);
             const float own_m = te->own_m, m = fmaxf(rest.m, own_m), base = m == neg_inf() ? 0.0f : m;
             const float down = ex2(fmaxf(rel_base(rest.m, base, p.c), kFloor));
             const float s = te->own_s * ex2(fmaxf(rel_base(own_m, base, p.c), kFloor)) + rest.s * down;
