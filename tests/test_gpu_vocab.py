@@ -262,6 +262,7 @@ def test_distill_lists_that_are_not_a_top(dtype, tail):
     x[7, ::2] = -INF
     x[7, index[7].long()] = 1.0
     x[8] = torch.finfo(dtype).min                  # equals
+    x[4, index[4, 3].long()] = -INF                # a token of the teacher that the student excludes: an infinite loss
     check_distill(x, index, logp, 1.0, tail)
 
 
