@@ -9,6 +9,9 @@ that a profiler can capture one or two launches of one kernel in a minute:
                         rounds of bcq_linear_decode_packed over them (default q = 4, n = 1)
     quantize [alt]      greedy (alt = 0, five 6400 x 1600 matrices) or greedy + alt alternating
                         rounds (five 5120 x 5120 matrices), q = 4, g = 128
+    logprobs [top]      1480 rows of 50257 bf16 logits, log probabilities and top alternatives (default 64)
+    distill             1776 such rows, distillation loss and gradient against 64 alternatives of a teacher
+    mx [n]              OPT-13B FFN up (5120 -> 20480) in microscaled 4-bit floating point, n tokens (default 2048)
 """
 import sys
 
@@ -70,6 +73,35 @@ def _quantize(alt):
         bcq.quantize(W, 4, 128, alt)
 
 
+def _logits(n, seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    return (torch.randn((n, 50304), generator=gen, device="cuda") * 2.0).bfloat16()[:, :50257]
+
+
+def _logprobs(top):
+    x = _logits(1480, 1)
+    for _ in range(3):
+        bcq.token_logprobs(x, top_k=top)
+
+
+def _distill():
+    x = _logits(1776, 1)
+    _, _, top, index = bcq.token_logprobs(_logits(1776, 2), top_k=64)
+    w = torch.full((1776,), 1.0 / 1776, device="cuda")
+    for _ in range(3):
+        bcq.distill_grad(x, index, top, w)
+
+
+def _mx(n):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    W = bcq.mx_quantize(torch.randn((20480, 5120), generator=gen, device="cuda") * 0.02)
+    X = torch.randn((n, 5120), generator=gen, device="cuda").bfloat16()
+    for _ in range(3):
+        bcq.mx_linear(X, W, out_dtype=torch.bfloat16)
+
+
 def main(argv):
     case = argv[1] if len(argv) > 1 else "fwd"
     if case in ("fwd", "dx", "dalpha"):
@@ -78,6 +110,12 @@ def main(argv):
         _decode(int(argv[2]) if len(argv) > 2 else 4, int(argv[3]) if len(argv) > 3 else 1)
     elif case == "quantize":
         _quantize(int(argv[2]) if len(argv) > 2 else 0)
+    elif case == "logprobs":
+        _logprobs(int(argv[2]) if len(argv) > 2 else 64)
+    elif case == "distill":
+        _distill()
+    elif case == "mx":
+        _mx(int(argv[2]) if len(argv) > 2 else 2048)
     else:
         raise SystemExit(__doc__)
     torch.cuda.synchronize()
