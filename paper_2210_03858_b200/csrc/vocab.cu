@@ -10,7 +10,7 @@
 // conversion, an exponential (16 a cycle and SM: 0.7 of the time its bytes take), half a product and half a sum for each
 // result (two at a time, fma.rn.f32x2), a quarter of a maximum and half a clamp, and with everything that goes with a row
 // 7.6 instructions (9.1 with products and sums one at a time).
-// Measured: 2048 rows of 50304 in fp32, no list, 64 us, 98 % of the rate of a copy; 4096 rows of 50257 in bf16, no list 69 us (92 %),
+// Measured: 2048 rows of 50304 in fp32, no list, 62 us, the rate of a copy; 4096 rows of 50257 in bf16, no list 66 us (95 %),
 // 64 alternatives 110; the loss of 2048 rows of 50272 in fp32 69 us (92 %), of 50257 in bf16 48 us (65 %), with the gradient 108 us
 // (58 %).
 //
@@ -415,6 +415,9 @@ __device__ __forceinline__ Stats join_row(const R& run, Stats* part, Stats* mine
 // ---------------------------------------------------------------- log probabilities
 
 constexpr int kLpThreads = 256;
+// Without a list smaller CTAs, which leave and come more evenly: 2048 rows of 50304, fp32, 64.0 and 61.4 us; 4096 of 50257, bf16, 68.7 and
+// 66.1.  (With one, the bound from 128 threads is too low for long lists: 128 alternatives 136 us, 1137 so.)
+constexpr int kLpThreadsPlain = 128;
 
 struct TopShared {
     unsigned long long cand[kCandidates];
@@ -594,9 +597,9 @@ __device__ __forceinline__ float log_prob(float x, float m, float log_s, const L
 }
 
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(kLpThreads)
+__global__ void __launch_bounds__(TOP ? kLpThreads : kLpThreadsPlain)
 token_logprobs_kernel(const T* logits, const LogprobParams p) {
-    constexpr int NT = kLpThreads;
+    constexpr int NT = TOP ? kLpThreads : kLpThreadsPlain;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ Stats part[NT / 32];
     __shared__ Stats mine;
@@ -627,7 +630,7 @@ token_logprobs_kernel(const T* logits, const LogprobParams p) {
     if (sh.single >= 0) run.one(single, p.c);
 
     // (first, so that the cluster meets once for the sums and the lists; of a row that is no distribution it comes to nothing)
-    if (TOP) top_of_share<T>(sh, p.top, run.m, single, batch_max, stream.batches(), ts);
+    if constexpr (TOP) top_of_share<T>(sh, p.top, run.m, single, batch_max, stream.batches(), ts);
     const Stats st = join_row<NT>(run, part, &mine, p.ctas, p.c);
     const bool none = st.bad || !(st.s > 0.0f);  // no distribution
     const float log_s = log2f(st.s);
@@ -1170,7 +1173,7 @@ bcq_status launch_logprobs(int n, const void* logits, LogprobParams p, cudaStrea
         if (st != BCQ_OK) return st;
         BCQ_CUDA_TRY(launch_pdl(token_logprobs_kernel<T, true>, grid, kLpThreads, smem, s, (unsigned)p.ctas, (const T*)logits, p));
     } else {
-        BCQ_CUDA_TRY(launch_pdl(token_logprobs_kernel<T, false>, grid, kLpThreads, 0, s, (unsigned)p.ctas, (const T*)logits, p));
+        BCQ_CUDA_TRY(launch_pdl(token_logprobs_kernel<T, false>, grid, kLpThreadsPlain, 0, s, (unsigned)p.ctas, (const T*)logits, p));
     }
     return BCQ_OK;
 }
@@ -1214,7 +1217,7 @@ extern "C" bcq_status bcq_token_logprobs(int n, int vocab, const void* logits, s
     p.targets = targets;
     p.c = exponent_scale(temperature); p.inv_t = 1.0f / temperature;
     p.logprob = logprob; p.entropy = entropy; p.top_logprob = top_logprob; p.top_index = top_index;
-    p.ctas = ctas_for(n, vocab, dtype == BCQ_BF16 ? 2 : 4, kLpThreads, 3);
+    p.ctas = top_k > 0 ? ctas_for(n, vocab, dtype == BCQ_BF16 ? 2 : 4, kLpThreads, 3) : ctas_for(n, vocab, dtype == BCQ_BF16 ? 2 : 4, kLpThreadsPlain, 6);
     p.lg = log2_of(p.ctas);
     cudaStream_t s = (cudaStream_t)stream;
     return dtype == BCQ_BF16 ? launch_logprobs<__nv_bfloat16>(n, logits, p, s) : launch_logprobs<float>(n, logits, p, s);
