@@ -55,7 +55,7 @@ extern "C" const char* bcq_status_string(int status) {
         case BCQ_ERR_NULL: return "a required pointer is NULL";
         case BCQ_ERR_SHAPE: return "a size or pitch is out of range";
         case BCQ_ERR_ALIGN: return "a pointer or pitch is not aligned as required";
-        case BCQ_ERR_UNSUPPORTED: return "shape not covered by the kernels (q > 8, or g neither d_in nor a multiple of 32)";
+        case BCQ_ERR_UNSUPPORTED: return "shape not covered by the kernels (q > 8, g neither d_in nor a multiple of 32, or another limit or type that bcq.h names)";
         case BCQ_ERR_WORKSPACE: return "workspace smaller than bcq_workspace_bytes()";
         case BCQ_ERR_CUDA: return "a CUDA call failed (see bcq_last_cuda_error)";
         case BCQ_ERR_DEVICE_TIMEOUT: return "a kernel gave up on a bounded wait";

@@ -186,6 +186,34 @@ def test_linear_takes_values_and_keeps_nan_apart():
     assert bcq.mx_linear(x[:0], W).shape == (0, 300)
 
 
+def test_operands_that_cannot_be_passed_on():
+    x = torch.randn((4, 64), device="cuda")
+    M = bcq.mx_quantize(x)
+    for bad, error in ((x.half(), TypeError), (x[0], ValueError), (x.t(), ValueError), (x.cpu(), ValueError), (3, TypeError)):
+        with pytest.raises(error):
+            bcq.mx_quantize(bad)
+    with pytest.raises(bcq.BcqError):
+        bcq.mx_quantize(x[:1].expand(4, 64))
+    with pytest.raises(ValueError):
+        bcq.MxMatrix(M.codes, M.scales, 4, 200)
+    with pytest.raises(ValueError):
+        bcq.MxMatrix(M.codes[:3], M.scales, 4, 64)
+    with pytest.raises(TypeError):
+        bcq.MxMatrix(M.codes.int(), M.scales, 4, 64)
+    with pytest.raises(ValueError):
+        bcq.mx_linear(M, bcq.mx_quantize(torch.randn((4, 65), device="cuda")))
+    with pytest.raises(TypeError):
+        bcq.mx_linear(M, M, out_dtype=torch.float16)
+    for bad, error in ((torch.zeros(5, device="cuda"), ValueError), (torch.zeros(4, device="cuda", dtype=BF16), TypeError)):
+        with pytest.raises(error):
+            bcq.mx_linear(M, M, bias=bad)
+    for bad, error in ((torch.zeros((4, 5), device="cuda"), ValueError), (torch.zeros((4, 4), device="cuda").half(), TypeError),
+                       (torch.zeros((4, 4), device="cuda").t()[:, ::1].t()[:, :4].t(), ValueError)):
+        with pytest.raises(error):
+            bcq.mx_linear(M, M, out=bad)
+    assert torch.equal(bcq.mx_linear(M, M), bcq.mx_linear(M, M, out=torch.empty((4, 4), device="cuda")))
+
+
 def test_mx_on_a_side_stream_and_in_a_graph():
     g = torch.Generator(device="cuda").manual_seed(4)
     x, x2 = (torch.randn((40, 1024), generator=g, device="cuda").bfloat16() for _ in range(2))

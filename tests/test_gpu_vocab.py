@@ -1,10 +1,10 @@
 """Operators over rows of logits -- log probabilities with entropy and top alternatives, the distillation loss and its gradient --
 against their formulas in 64 bits.
 
-Tolerances.  A thread adds up at most vocab / 512 + 8 pairs of exponentials, each addition of positive terms within 2^-24 of the
+Tolerances.  A thread (of 128 at least) adds up at most vocab / 256 + 8 pairs of exponentials, each addition of positive terms within 2^-24 of the
 result; the sums of threads, warps and CTAs are joined in at most 24 steps of three operations; an exponential is within 2^-22, its
 argument (three roundings of a number up to |z|) within 3 |z| 2^-24.  So a row's sum S is within
-    eps_s = (vocab / 512 + 8 + 72) 2^-24 + 2^-22 + 3 z 2^-24,  z <= 40: what lies lower adds less than 2^-40
+    eps_s = (vocab / 256 + 8 + 72) 2^-24 + 2^-22 + 3 z 2^-24,  z <= 40: what lies lower adds less than 2^-40
 of itself, a log probability within eps_s + 4 |lp| 2^-24, the entropy log S - sum(e z) / S within 4 eps_s (1 + H).  A gradient element
 w / T (q P - p) is within (2 eps_s + 2^-20) |w| / T max(q P, p), plus half a step of its type.  The loss is computed in 64 bits from S
 and the logits, where an error of S moves it by eps_s sum|p - q| <= 2 eps_s: near the minimum by less."""
@@ -29,7 +29,7 @@ def _built():
 
 
 def eps_s(vocab):
-    return (vocab / 512 + 80) * 2.0 ** -24 + 2.0 ** -22 + 120 * 2.0 ** -24
+    return (vocab / 256 + 80) * 2.0 ** -24 + 2.0 ** -22 + 120 * 2.0 ** -24
 
 
 def make_logits(n, vocab, dtype, pad=0, offset=0, seed=0, scale=3.0):
@@ -238,7 +238,7 @@ def test_distill_layouts(dtype, vocab, pad, offset):
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("vocab", [262144, 393216])
 def test_distill_largest_vocabularies(dtype, vocab):
-    for n in (2, 150):
+    for n in (2, 150, 460):  # (the last: a CTA has a whole row, and an SM room for one CTA)
         x = make_logits(n, vocab, dtype, seed=n)
         check_distill(x, *teacher_of(x, 128, 1.0), 1.0, True)
     check_logprobs(x, None, 128)
@@ -365,6 +365,52 @@ def test_cross_entropy_is_a_list_of_one():
     ref = torch.softmax(x.double(), dim=1)
     ref[torch.arange(37), label[:, 0]] -= 1
     assert float((d.double() - ref / 37).abs().max()) <= (2.0 ** -8 * 1.01 + 4 * eps_s(50257)) / 37
+
+
+@pytest.mark.parametrize("call", ["logprobs", "loss", "grad"])
+def test_operands_that_cannot_be_passed_on(call):
+    x = make_logits(3, 50, F32)
+    index, logp = teacher_of(x, 4, 1.0)
+    w, t = torch.ones(3, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda")
+    f = {"logprobs": lambda x=x, t=t, k=2, **kw: bcq.token_logprobs(x, t, top_k=k, **kw),
+         "loss": lambda x=x, index=index, logp=logp, **kw: bcq.distill_loss(x, index, logp, **kw),
+         "grad": lambda x=x, index=index, logp=logp, w=w, **kw: bcq.distill_grad(x, index, logp, w, **kw)}[call]
+    f()
+    for bad in (x.half(), x.double(), "logits"):
+        with pytest.raises(TypeError):
+            f(x=bad)
+    for bad in (x[0], x.t(), x[:, ::2], x.cpu()):
+        with pytest.raises(ValueError):
+            f(x=bad)
+    for T in (0.0, float("nan"), 1e9):
+        with pytest.raises(bcq.BcqError):
+            f(temperature=T)
+    with pytest.raises(bcq.BcqError):
+        f(x=x[:1].expand(3, 50))            # rows on top of each other
+    if call == "logprobs":
+        for bad, error in ((t.int(), TypeError), (t[:2], ValueError), (t.cpu(), ValueError), (t.repeat(2)[::2], ValueError)):
+            with pytest.raises(error):
+                f(t=bad)
+        for k in (-1, 129):
+            with pytest.raises(bcq.BcqError):
+                f(k=k)
+    else:
+        for bad, error in ((index.long(), TypeError), (index[:2], ValueError), (index[0], ValueError), (index.cpu(), ValueError), (index[:, :2], ValueError)):
+            with pytest.raises(error):
+                f(index=bad)
+        for bad, error in ((logp.double(), TypeError), (logp[:, :3].contiguous(), ValueError)):
+            with pytest.raises(error):
+                f(logp=bad)
+        with pytest.raises(bcq.BcqError):
+            f(index=index[:, :0].contiguous(), logp=logp[:, :0].contiguous())
+    if call == "grad":
+        for bad, error in ((w[:2], ValueError), (w.double(), TypeError)):
+            with pytest.raises(error):
+                f(w=bad)
+        for bad, error in ((torch.empty((3, 51), device="cuda"), ValueError), (torch.empty((3, 50), device="cuda", dtype=BF16), TypeError),
+                           (torch.empty((50, 3), device="cuda").t(), ValueError)):
+            with pytest.raises(error):
+                f(out=bad)
 
 
 # ---------------------------------------------------------------- streams and graphs
