@@ -275,7 +275,8 @@ struct Running {
 // Goes through the vectors of a share, kBatch of a thread at a time, each batch on its way while the one before it is used:
 // use(whole, b, v, have) gets batch b, of which this thread has the first `have` vectors.  The last, incomplete batch
 // comes first: the loop has whole ones only, without a condition on any load.  start() sends for the first two.
-template <typename T, int NT>
+// AGAIN: the share is read a second time, last batches first: the loads leave it in L1 and L2 as far as there is room.
+template <typename T, int NT, bool AGAIN = false>
 struct Stream {
     const uint4* at;
     int whole, rest;  // whole batches, vectors of this thread in the incomplete one
@@ -292,18 +293,46 @@ struct Stream {
     __device__ __forceinline__ int batches() const { return whole + (more ? 1 : 0); }
     __device__ __forceinline__ void load(int b, uint4 (&v)[kBatch]) const {
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) v[u] = ld_stream(at + b * (kBatch * NT) + u * NT);
+        for (int u = 0; u < kBatch; ++u) {
+            const uint4* from = at + b * (kBatch * NT) + u * NT;
+            v[u] = AGAIN ? ld(from) : ld_stream(from);
+        }
     }
     __device__ __forceinline__ void load_rest(uint4 (&v)[kBatch]) const {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
             v[u] = make_uint4(Elem<T>::kMasked, Elem<T>::kMasked, Elem<T>::kMasked, Elem<T>::kMasked);
-            if (u < rest) v[u] = ld_stream(at + whole * (kBatch * NT) + u * NT);
+            const uint4* from = at + whole * (kBatch * NT) + u * NT;
+            if (u < rest) v[u] = AGAIN ? ld(from) : ld_stream(from);
         }
     }
     __device__ __forceinline__ void start(uint4 (&a)[kBatch], uint4 (&b)[kBatch]) const {
         if (more) load_rest(a);
         if (whole > 0) load(0, b);
+    }
+    // Backwards: the last whole batch first, the incomplete one last.
+    __device__ __forceinline__ void load_back(int i, uint4 (&v)[kBatch]) const {
+        if (i < whole) load(whole - 1 - i, v);
+        else if (more) load_rest(v);
+    }
+    __device__ __forceinline__ void start_back(uint4 (&a)[kBatch], uint4 (&b)[kBatch]) const {
+        load_back(0, a);
+        if (batches() > 1) load_back(1, b);
+    }
+    template <typename Use>
+    __device__ __forceinline__ void run_back(uint4 (&a)[kBatch], uint4 (&b)[kBatch], Use use) const {
+        for (int i = 0; i < whole; i += 2) {
+            use(std::true_type(), whole - 1 - i, a, kBatch);
+            if (i + 2 < batches()) load_back(i + 2, a);
+            if (i + 1 < whole) {
+                use(std::true_type(), whole - 2 - i, b, kBatch);
+                if (i + 3 < batches()) load_back(i + 3, b);
+            }
+        }
+        if (more) {
+            if (whole & 1) use(std::false_type(), whole, b, rest);
+            else use(std::false_type(), whole, a, rest);
+        }
     }
     template <typename Use>
     __device__ __forceinline__ void run(uint4 (&a)[kBatch], uint4 (&b)[kBatch], Use use) const {
@@ -1031,10 +1060,10 @@ distill_kernel(const T* logits, T* grad, const DistillParams p) {
         }
     } else if (row < p.n) {
         uint4 va[kBatch], vb[kBatch];
-        Stream<T, NT>(share(row)).start(va, vb);
+        Stream<T, NT, GRAD>(share(row)).start(va, vb);
         for (int it = 0; row < p.n; row += step, ++it) {
             const Share<T> sh = share(row);
-            const Stream<T, NT> stream(sh);
+            const Stream<T, NT, GRAD> stream(sh);
             const float single = sh.single >= 0 ? Elem<T>::get(sh.row + sh.single) : 0.0f;
             Teacher* te = &teachers[it & 1];
             const uint8_t* mark = reinterpret_cast<const uint8_t*>(marks) + (it & 1) * p.marks_bytes;
@@ -1058,7 +1087,7 @@ distill_kernel(const T* logits, T* grad, const DistillParams p) {
             }
             // what comes next is on its way while the sums are joined: the row again, or the next one
             const int next = row + step;
-            if (GRAD) stream.start(va, vb);
+            if (GRAD) stream.start_back(va, vb);
             else if (next < p.n) Stream<T, NT>(share(next)).start(va, vb);
             const Stats rest = join_row<NT>(run, part, &mine[it & 1], p.ctas, p.c);
             ptx::named_bar_sync(kListed + (it & 1), NT + 32);
@@ -1094,7 +1123,7 @@ distill_kernel(const T* logits, T* grad, const DistillParams p) {
                         out[j] = from_float<T>(ex2((Elem<T>::get(sh.row + j) - m_rest) * p.c) * f_rest);
                 } else if (((reinterpret_cast<uintptr_t>(out + sh.head) ^ reinterpret_cast<uintptr_t>(sh.row + sh.head)) & 15u) == 0) {
                     uint4* out_vec = reinterpret_cast<uint4*>(out + sh.head) + sh.v0 + tid;
-                    stream.run(va, vb, [&](auto whole, int b, uint4(&v)[kBatch], int have) {
+                    stream.run_back(va, vb, [&](auto whole, int b, uint4(&v)[kBatch], int have) {
 #pragma unroll
                         for (int u = 0; u < kBatch; ++u)
                             if (decltype(whole)::value || u < have) st_stream(out_vec + b * (kBatch * NT) + u * NT, g(v[u]));
@@ -1107,7 +1136,7 @@ distill_kernel(const T* logits, T* grad, const DistillParams p) {
                     const int before = (int)(((16u - (uint32_t)(reinterpret_cast<uintptr_t>(out + from) & 15u)) & 15u) / sizeof(T));
                     const int count = max(0, sh.v1 - sh.v0 - 1);
                     uint4* out_vec = reinterpret_cast<uint4*>(out + from + before);
-                    for (int v = tid; v < count; v += kBatch * NT) {
+                    for (int v = (count - 1) / (kBatch * NT) * (kBatch * NT) + tid; v >= 0; v -= kBatch * NT) {
                         const uint4* at = sh.vec(sh.v0 + v);  // (a neighbour's vector is in L1 by then, or on its way)
 #pragma unroll
                         for (int u = 0; u < kBatch; ++u)
@@ -1123,7 +1152,7 @@ distill_kernel(const T* logits, T* grad, const DistillParams p) {
                     for (int j = sh.first + tid; j < min(lo, sh.last); j += NT) out[j] = from_float<T>(g(Elem<T>::get(sh.row + j)));
                     for (int j = hi + tid; count > 0 && j < sh.last; j += NT) out[j] = from_float<T>(g(Elem<T>::get(sh.row + j)));
                 }
-                if (next < p.n) Stream<T, NT>(share(next)).start(va, vb);
+                if (next < p.n) Stream<T, NT, GRAD>(share(next)).start(va, vb);
                 row_sync<NT>();
                 if (tid < p.k && te->first[tid] && te->index[tid] >= sh.first && te->index[tid] < sh.last) {
                     const float q = ex2(rel(te->x[tid], base, p.c)) * f_own;
