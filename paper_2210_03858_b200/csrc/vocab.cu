@@ -11,7 +11,7 @@
 // result (two at a time, fma.rn.f32x2), a quarter of a maximum and half a clamp, and with everything that goes with a row
 // 7.6 instructions (9.1 with products and sums one at a time).
 // Measured: 2048 rows of 50304 in fp32, no list, 62 us, the rate of a copy; 4096 rows of 50257 in bf16, no list 66 us (95 %),
-// 64 alternatives 110; the loss of 2048 rows of 50272 in fp32 69 us (92 %), of 50257 in bf16 48 us (65 %), with the gradient 94 us
+// 64 alternatives 103; the loss of 2048 rows of 50272 in fp32 69 us (92 %), of 50257 in bf16 48 us (65 %), with the gradient 94 us
 // (67 %).
 //
 // Rows start at any element (an odd vocabulary in bf16 leaves rows at odd addresses): the elements before the
@@ -625,9 +625,13 @@ __device__ __forceinline__ float log_prob(float x, float m, float log_s, const L
     return (x - m) * p.inv_t - log_s * kLn2;
 }
 
-template <typename T, bool TOP>
-__global__ void __launch_bounds__(TOP ? kLpThreads : kLpThreadsPlain)
+// LIST 0: none; 1: a short one; 2: a long one, of which more batches are read again, so that the first reading leaves them in L1 as
+// far as there is room (4096 rows of 50257, bf16: 128 alternatives 136 us past L1 and 122 so, 64 110 and 103, 20 86 and 92).
+constexpr int kLongList = 32;
+template <typename T, int LIST>
+__global__ void __launch_bounds__(LIST ? kLpThreads : kLpThreadsPlain)
 token_logprobs_kernel(const T* logits, const LogprobParams p) {
+    constexpr bool TOP = LIST != 0;
     constexpr int NT = TOP ? kLpThreads : kLpThreadsPlain;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ Stats part[NT / 32];
@@ -649,7 +653,7 @@ token_logprobs_kernel(const T* logits, const LogprobParams p) {
     const float single = sh.single >= 0 ? Elem<T>::get(sh.row + sh.single) : neg_inf();
 
     Running<T, true> run;
-    const Stream<T, NT> stream(sh);
+    const Stream<T, NT, LIST == 2> stream(sh);
     uint4 va[kBatch], vb[kBatch];
     stream.start(va, vb);
     stream.run(va, vb, [&](auto whole, int b, uint4(&v)[kBatch], int have) {
@@ -1192,19 +1196,23 @@ int log2_of(int ctas) { return ctas == 8 ? 3 : ctas / 2; }
 
 int max_vectors(int vocab, int elem_bytes, int ctas) { return ceil_div(vocab * elem_bytes / 16, ctas); }
 
-template <typename T>
-bcq_status launch_logprobs(int n, const void* logits, LogprobParams p, cudaStream_t s) {
+template <typename T, int LIST>
+bcq_status launch_logprobs_as(int n, const void* logits, const LogprobParams& p, cudaStream_t s) {
     const int nv = max_vectors(p.vocab, (int)sizeof(T), p.ctas);
-    const size_t smem = p.top > 0 ? sizeof(TopShared) + (size_t)ceil_div(nv, kBatch * kLpThreads) * kLpThreads * 4 : 0;
-    const dim3 grid((unsigned)(n * p.ctas));
-    if (p.top > 0) {
-        const bcq_status st = ensure_dynamic_smem(token_logprobs_kernel<T, true>, smem);
+    const size_t smem = LIST ? sizeof(TopShared) + (size_t)ceil_div(nv, kBatch * kLpThreads) * kLpThreads * 4 : 0;
+    if (LIST) {
+        const bcq_status st = ensure_dynamic_smem(token_logprobs_kernel<T, LIST>, smem);
         if (st != BCQ_OK) return st;
-        BCQ_CUDA_TRY(launch_pdl(token_logprobs_kernel<T, true>, grid, kLpThreads, smem, s, (unsigned)p.ctas, (const T*)logits, p));
-    } else {
-        BCQ_CUDA_TRY(launch_pdl(token_logprobs_kernel<T, false>, grid, kLpThreadsPlain, 0, s, (unsigned)p.ctas, (const T*)logits, p));
     }
+    BCQ_CUDA_TRY(launch_pdl(token_logprobs_kernel<T, LIST>, dim3((unsigned)(n * p.ctas)), LIST ? kLpThreads : kLpThreadsPlain, smem, s,
+                            (unsigned)p.ctas, (const T*)logits, p));
     return BCQ_OK;
+}
+
+template <typename T>
+bcq_status launch_logprobs(int n, const void* logits, const LogprobParams& p, cudaStream_t s) {
+    if (p.top == 0) return launch_logprobs_as<T, 0>(n, logits, p, s);
+    return p.top > kLongList ? launch_logprobs_as<T, 2>(n, logits, p, s) : launch_logprobs_as<T, 1>(n, logits, p, s);
 }
 
 template <typename T, bool GRAD>
