@@ -152,7 +152,7 @@ struct EightOf<float> { typedef EightF32 type; };
 template <>
 struct EightOf<__nv_bfloat16> { typedef EightBf16 type; };
 
-// Bound by memory: 16384 x 4096 fp32 values 52 us, 5.8 TB/s.
+// Bound by memory: 16384 x 4096 fp32 values 49 us, 6.1 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(256)
 mx_quantize_kernel(const T* X, uint8_t* codes, uint32_t* scales, const MxQuantParams p) {
@@ -213,7 +213,7 @@ __device__ __forceinline__ void four_values(uint32_t c, uint32_t scale, uint32_t
     asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(v23) : "r"(scale));
 }
 
-// Bound by memory too.  (With every code put together as a float, 16 instructions an element, 43 us for 16384 x 4096; 27 so.)
+// Bound by memory too.  (With every code put together as a float, 16 instructions an element, 43 us for 16384 x 4096; 33 so, 5.1 TB/s.)
 template <typename T>
 __global__ void __launch_bounds__(256)
 mx_dequantize_kernel(const uint8_t* codes, const uint32_t* scales, T* X, const MxQuantParams p) {
