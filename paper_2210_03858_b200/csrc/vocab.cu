@@ -888,10 +888,12 @@ __device__ __forceinline__ void prepare_row(const DistillParams& p, const Share<
 
 // What a class adds to the divergence, p (d + expm1(-d)) with d = log p - log q: never negative, so near distributions lose
 // nothing to the cancellation of p log p against p log q, and a common error of all log q (that of the row's sum) drops
-// out.  In 64 bits: k + 1 values a row.
+// out.  In 64 bits: k + 1 values a row.  Where q is far larger than p nothing cancels, and p e^-d is q: there p may be a
+// subnormal number next to which e^-d overflows (log p below -709).
 __device__ __forceinline__ double class_loss(double p, double log_p, double log_q) {
     if (!(p > 0.0)) return p == 0.0 ? exp(log_q) : p;
     const double d = log_p - log_q;
+    if (d < -30.0) return p * (d - 1.0) + exp(log_q);
     return p * (d + expm1(-d));
 }
 
