@@ -936,8 +936,10 @@ __device__ __forceinline__ float from_float<float>(float x) { return x; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
-// The gradient of a token that the teacher does not name, f 2^(c x - b).  In bf16 the magnitude of f is part of the exponent (its
-// logarithm is off by 2^-24 of itself, some 2^-19 of the result), which saves a product: the sign is left.
+// The gradient of a token that the teacher does not name, f 2^(c x - b).  In bf16 the magnitude of f is part of the exponent, which
+// saves a product: the sign is left.  The sum log2|f| - b is rounded, so this is done only where it is below 2^10: the result is off by
+// 2^-15 of itself then, a hundredth of half a step (and by the error of the logarithm, 2^-18).  fits() says whether it is; a row
+// where it is not (c max x beyond 1000 or so) goes to rest_of_row().
 template <typename T>
 struct RestGrad {
     float c, nb, f;  // bf16: f is 1 or -1
@@ -949,6 +951,8 @@ struct RestGrad {
             f = f < 0.0f ? -1.0f : 1.0f;
         }
     }
+    // (-inf: all are zero; NaN: all are)
+    __device__ __forceinline__ bool fits() const { return sizeof(T) == 4 || !(fabsf(nb) > 1024.0f) || nb == neg_inf(); }
     __device__ __forceinline__ float operator()(float x) const { return ex2(fmaf(x, c, nb)) * f; }
     // of a vector
     __device__ __forceinline__ uint4 operator()(const uint4& x) const {
@@ -1010,6 +1014,28 @@ __device__ __forceinline__ void zero_row(T* out, int first, int last, int tid, i
     for (int v = tid; v < count; v += threads) st_stream(reinterpret_cast<uint4*>(out + from) + v, make_uint4(0u, 0u, 0u, 0u));
     if (tid < before) out[first + tid] = from_float<T>(0.0f);
     if (tid < last - after) out[after + tid] = from_float<T>(0.0f);
+}
+
+// The gradient of the tokens that the teacher does not name, all of this CTA's share, where RestGrad does not do: f 2^rel(x, m), element
+// by element, in whole vectors where logits and result have them at the same places.
+template <typename T>
+__device__ __noinline__ void rest_of_row(const Share<T> sh, T* out, float m, float f, float c, int tid, int threads) {
+    constexpr int E = Elem<T>::E;
+    auto grad = [&](float x) { return from_float<T>(ex2(rel(x, m, c)) * f); };
+    if (((reinterpret_cast<uintptr_t>(out + sh.head) ^ reinterpret_cast<uintptr_t>(sh.row + sh.head)) & 15u) == 0) {
+        for (int v = sh.v0 + tid; v < sh.v1; v += threads) {
+            const uint4 x = ld(sh.vec(v));
+            T y[E];
+#pragma unroll
+            for (int i = 0; i < E; ++i) y[i] = grad(Elem<T>::at(x, i));
+            uint4 w;
+            memcpy(&w, y, 16);
+            st_stream(reinterpret_cast<uint4*>(out + sh.head) + v, w);
+        }
+        if (sh.single >= 0) out[sh.single] = grad(Elem<T>::get(sh.row + sh.single));
+    } else {
+        for (int j = sh.first + tid; j < sh.last; j += threads) out[j] = grad(Elem<T>::get(sh.row + j));
+    }
 }
 
 constexpr int kDistillThreads = 256;  // that go through a row; one more warp helps them
@@ -1124,9 +1150,8 @@ distill_kernel(const T* logits, T* grad, const DistillParams p) {
                 // (the teacher's tokens, whose exponent may overflow here, are written after the others)
                 if (zero) {
                     zero_row(out, sh.first, sh.last, tid, NT);
-                } else if (far) {
-                    for (int j = sh.first + tid; j < sh.last; j += NT)
-                        out[j] = from_float<T>(ex2((Elem<T>::get(sh.row + j) - m_rest) * p.c) * f_rest);
+                } else if (far || !g.fits()) {
+                    rest_of_row<T>(sh, out, m_rest, f_rest, p.c, tid, NT);
                 } else if (((reinterpret_cast<uintptr_t>(out + sh.head) ^ reinterpret_cast<uintptr_t>(sh.row + sh.head)) & 15u) == 0) {
                     uint4* out_vec = reinterpret_cast<uint4*>(out + sh.head) + sh.v0 + tid;
                     stream.run_back(va, vb, [&](auto whole, int b, uint4(&v)[kBatch], int have) {

@@ -10,7 +10,7 @@ import pytest
 
 import paper_2210_03858_b200 as bcq
 from paper_2210_03858_b200 import build as bcq_build
-from test_gpu_vocab import close, eps_s, make_logits, ref_distill, teacher_of
+from test_gpu_vocab import check_logprobs, close, eps_s, make_logits, ref_distill, teacher_of
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -38,6 +38,38 @@ def check_distill(x, index, logp, T, tail, w=None):
     half = torch.finfo(x.dtype).eps / 2
     close(d, grad * wd, (2 * e + 2.0 ** -20) * size * wd.abs() + half * (grad * wd).abs() * 1.01 + 2.0 ** -125 * (wd.abs() / T).clamp(min=1.0))
     return loss, d
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("tail", [True, False])
+def test_distill_gradient_of_large_logits(dtype, tail):
+    # |c m| from 2^5 to 2^24, of the whole row and of the tokens outside the list
+    for n, vocab in ((2, 50257), (300, 3001)):
+        x = make_logits(n, vocab, dtype, seed=11)
+        index, logp = teacher_of(x, 16, 1.0)
+        for size in (20.0, 300.0, 700.0, 1000.0, 3e4, 1e5, 1e6, 1e7):
+            for y in ((x.float() + size).to(dtype), (x.float() - size).to(dtype), (x.float() - size).to(dtype).scatter(1, index.long(), x.gather(1, index.long()))):
+                check_distill(y, index, logp, 1.0, tail)
+                check_distill(y, index, torch.log_softmax(logp, dim=1) - 1e-6, 1.0, tail)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T", [1 / 512, 1 / 64, 512.0])
+def test_temperatures_near_both_ends(dtype, T):
+    for n, vocab in ((3, 50257), (400, 4001)):
+        x = make_logits(n, vocab, dtype, pad=3, seed=13, scale=5.0)
+        targets = torch.arange(n, device="cuda")
+        check_logprobs(x, targets, 64, T)
+        index, logp = teacher_of(x, 100, T)     # (log probabilities down to some -10000)
+        for tail in (True, False):
+            check_distill(x, index, logp, T, tail)
+        # rows whose results are in another place than the logits': single elements and vectors
+        buf = torch.empty((n, vocab + 9), dtype=dtype, device="cuda")
+        w = torch.rand(n, device="cuda")
+        _, d = bcq.distill_grad(x, index, logp, w, T)
+        for shift in (0, 1, 2):
+            assert torch.equal(bcq.distill_grad(x, index, logp, w, T, out=buf[:, shift:shift + vocab])[1], d)
+        assert torch.equal(bcq.distill_grad(x, index, logp, w, T, out=x)[1], d)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
