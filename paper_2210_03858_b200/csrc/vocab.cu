@@ -5,8 +5,8 @@
 // for its sums (and the gradient's once more, from L2 as far as it is still there): a thread keeps a running maximum and the sums that go with it, and rescales them when a batch of its
 // vectors has a larger one, so no second pass is needed for the sums; the sums of threads, warps and CTAs are joined in
 // a fixed order.  b is the rounded product and is subtracted everywhere (from a target, from an alternative), so its
-// rounding error, which would be that of a probability, drops out.  What bounds them is memory: n vocab sizeof(T)
-// bytes read (and written, for the gradient).  Next to that is the issue of instructions: an element of bf16 costs a
+// rounding error, which would be that of a probability, drops out (where it would be too large for that, |b| > 2^20, exponents
+// are c (x - max x)).  What bounds them is memory: n vocab sizeof(T) bytes read (and written, for the gradient).  Next to that is the issue of instructions: an element of bf16 costs a
 // conversion, an exponential (16 a cycle and SM: 0.7 of the time its bytes take), half a product and half a sum for each
 // result (two at a time, fma.rn.f32x2), a quarter of a maximum and half a clamp, and with everything that goes with a row
 // 7.6 instructions (9.1 with products and sums one at a time).
@@ -82,17 +82,29 @@ __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
     return r;
 }
 
-// Logits beyond this, either way, are taken apart from the rest: c x may overflow.  Below -kFar times two a logit next to one
-// within kFar is as good as -kFar times two.
-constexpr float kFar = 6.338253e29f;  // 2^99
+// The base of a sum with maximum m is the rounded product b = rn(m c) where it is at most this either way, and m c itself beyond, with
+// exponents (x - m) c.  Subtracting b from c x leaves b's rounding error in the exponent, 2^-5 at most: the same for all terms, so it
+// drops out; of a product of 1e10 it would be hundreds, and the sum infinite or 0.
+constexpr float kNear = 1048576.0f;  // 2^20
+// Logits below this are as good as this one next to a base that is near, and times c it is finite.
+constexpr float kLowest = -1.26765060e30f;  // -2^100
 
-// Exponent of 2 of an element x relative to the maximum m, and that of a sum relative to the maximum a when it is taken
-// to the maximum m.  The rounded product m c is what is subtracted, each time the same number.
+__device__ __forceinline__ bool is_near(float b) { return fabsf(b) <= kNear; }  // (not so for an infinite m)
+
+// Exponent of 2 of an element x relative to the base of m, and that of a sum at the base of a when it is taken to the base of m,
+// exactly what lies between the two bases.
 __device__ __forceinline__ float rel(float x, float m, float c) {
-    return fabsf(m) <= kFar ? fmaf(fmaxf(x, -2.0f * kFar), c, -__fmul_rn(m, c)) : (x - m) * c;
+    const float b = __fmul_rn(m, c);
+    return is_near(b) ? fmaf(fmaxf(x, kLowest), c, -b) : (x - m) * c;
 }
+// What a near base leaves of m c (0 for one that is not near).
+__device__ __forceinline__ float base_error(float m, float c) {
+    const float b = __fmul_rn(m, c), e = fmaf(m, c, -b);
+    return is_near(b) ? e : 0.0f;
+}
+// (without a branch: a row goes through some twenty of these one after the other)
 __device__ __forceinline__ float rel_base(float a, float m, float c) {
-    return fabsf(a) <= kFar && fabsf(m) <= kFar ? __fsub_rn(__fmul_rn(a, c), __fmul_rn(m, c)) : (a - m) * c;
+    return (a - m) * c + (base_error(m, c) - base_error(a, c));
 }
 
 // ---------------------------------------------------------------- element types
@@ -114,10 +126,10 @@ struct Elem<float> {
         return max_nan(max_nan(max_of(v[0]), max_of(v[1])), max_nan(max_of(v[2]), max_of(v[3])));
     }
     static __device__ __forceinline__ void clamp(uint4& v) {
-        v.x = __float_as_uint(fmaxf(__uint_as_float(v.x), -2.0f * kFar));
-        v.y = __float_as_uint(fmaxf(__uint_as_float(v.y), -2.0f * kFar));
-        v.z = __float_as_uint(fmaxf(__uint_as_float(v.z), -2.0f * kFar));
-        v.w = __float_as_uint(fmaxf(__uint_as_float(v.w), -2.0f * kFar));
+        v.x = __float_as_uint(fmaxf(__uint_as_float(v.x), kLowest));
+        v.y = __float_as_uint(fmaxf(__uint_as_float(v.y), kLowest));
+        v.z = __float_as_uint(fmaxf(__uint_as_float(v.z), kLowest));
+        v.w = __float_as_uint(fmaxf(__uint_as_float(v.w), kLowest));
     }
     static __device__ __forceinline__ void mask(uint4& v, uint32_t bits) {
         if (bits & 1u) v.x = kMasked;
@@ -194,7 +206,7 @@ struct Share {
     __device__ __forceinline__ const uint4* vec(int v) const { return reinterpret_cast<const uint4*>(row + head) + v; }
 };
 
-// Sums of e and e z over a vector of a row that lies far out as a whole, or holds nothing so far.
+// Sums of e and e z over a vector where the base is not near, or the thread has found nothing above -inf so far.
 template <typename T>
 __device__ __noinline__ float2 far_sums(uint4 v, float m, float c) {
     const float base = m == neg_inf() ? 0.0f : m;
@@ -253,8 +265,8 @@ struct Running {
     __device__ __forceinline__ float batch(const uint4 (&v)[kBatch], int have, float c) {
         const float x = Elem<T>::max_of4(v);
         raise(x, c);
-        if (fabsf(m) <= kFar) {
-            const float nb = -__fmul_rn(m, c);
+        const float nb = -__fmul_rn(m, c);
+        if (is_near(nb)) {
 #pragma unroll
             for (int u = 0; u < kBatch; ++u)
                 if (WHOLE || u < have) add_near(v[u], c, nb);
@@ -619,9 +631,9 @@ struct LogprobParams {
     int* top_index;
 };
 
-// (where the exponent of 2 may overflow, that of e may not)
+// (of a logit that is not one of the sum's near base, and where the exponent of 2 may overflow, that of e does not)
 __device__ __forceinline__ float log_prob(float x, float m, float log_s, const LogprobParams& p) {
-    if (fabsf(x) <= kFar && fabsf(m) <= kFar) return (rel(x, m, p.c) - log_s) * kLn2;
+    if (x >= kLowest && is_near(__fmul_rn(m, p.c))) return (rel(x, m, p.c) - log_s) * kLn2;
     return (x - m) * p.inv_t - log_s * kLn2;
 }
 
@@ -758,7 +770,6 @@ struct DistillParams {
     const float* logp;
     const float* dloss;
     float c, inv_t;
-    double inv_t64;
     float* loss;
 };
 
@@ -897,15 +908,12 @@ __device__ __forceinline__ double class_loss(double p, double log_p, double log_
     return p * (d + expm1(-d));
 }
 
-// Logarithms of e^(x / T), and of a sum's e^(a / T), relative to the base of a sum at m.
-__device__ __forceinline__ double log_rel(float x, float m, const DistillParams& p) {
-    if (fabsf(m) > kFar) return ((double)x - (double)m) * p.inv_t64;
-    return ((double)x * (double)p.c - (double)__fmul_rn(m, p.c)) * 0.69314718055994530942;
+// The base of a sum in 64 bits, where products of two floats are exact, and the logarithm of e^(x / T) relative to it.
+__device__ __forceinline__ double base_of(float m, float c) {
+    const float b = __fmul_rn(m, c);
+    return is_near(b) ? (double)b : (double)m * (double)c;
 }
-__device__ __forceinline__ double log_rel_base(float a, float m, const DistillParams& p) {
-    if (fabsf(a) > kFar || fabsf(m) > kFar) return ((double)a - (double)m) * p.inv_t64;
-    return ((double)__fmul_rn(a, p.c) - (double)__fmul_rn(m, p.c)) * 0.69314718055994530942;
-}
+__device__ __forceinline__ double log_rel(float x, double base, float c) { return ((double)x * (double)c - base) * 0.69314718055994530942; }
 
 // Loss of a row whose sums are there.  One warp.
 __device__ __forceinline__ float loss_of_row(const DistillParams& p, const Teacher* te) {
@@ -915,15 +923,16 @@ __device__ __forceinline__ float loss_of_row(const DistillParams& p, const Teach
     const double mass = p.tail ? total : (total == 0.0 ? 0.0 : total * keep);
     const double r = p.tail && te->s_rest > 0.0f ? fmax(0.0, 1.0 - mass) : 0.0;
     const double log_s = log((double)te->s), log_keep = p.tail || mass == 0.0 ? 0.0 : log(keep);
+    const double base = base_of(te->m, p.c);
     double loss = 0.0;
     for (int i = lane; i < p.k; i += 32) {
         if (te->index[i] < 0) continue;
-        const double log_q = log_rel(te->x[i], te->m, p) - log_s;
+        const double log_q = log_rel(te->x[i], base, p.c) - log_s;
         loss += class_loss(te->p[i] * keep, (double)te->logp[i] + log_keep, log_q);
         if (!te->first[i]) loss -= exp(log_q);  // its q counts once
     }
     loss = warp_sum(loss);
-    const double log_rho = log_rel_base(te->m_rest, te->m, p) + log((double)te->s_rest) - log_s;
+    const double log_rho = (base_of(te->m_rest, p.c) - base) * 0.69314718055994530942 + log((double)te->s_rest) - log_s;
     loss += class_loss(r, log(r), log_rho) + (mass + r - 1.0);
     if (mass == 0.0 && r == 0.0) loss = 0.0;  // the teacher says nothing
     return te->none ? quiet_nan() : (float)loss;
@@ -1143,14 +1152,14 @@ distill_kernel(const T* logits, T* grad, const DistillParams p) {
                 const bool zero = w == 0.0f;
                 const float r = rest.s > 0.0f ? te->r : 0.0f, f = w * p.inv_t, mass = te->mass + r;
                 const float f_rest = none ? quiet_nan() : f * (mass * (down / s) - (r > 0.0f ? r / rest.s : 0.0f));
-                const RestGrad<T> g(f_rest, p.c, __fmul_rn(m_rest, p.c));
-                const bool far = fabsf(m_rest) > kFar;
+                const float b_rest = __fmul_rn(m_rest, p.c);
+                const RestGrad<T> g(f_rest, p.c, b_rest);
                 const float f_own = none ? quiet_nan() : f * mass / s;
                 T* out = grad + (long long)row * p.ldd;
                 // (the teacher's tokens, whose exponent may overflow here, are written after the others)
                 if (zero) {
                     zero_row(out, sh.first, sh.last, tid, NT);
-                } else if (far || !g.fits()) {
+                } else if (!is_near(b_rest) || !g.fits()) {
                     rest_of_row<T>(sh, out, m_rest, f_rest, p.c, tid, NT);
                 } else if (((reinterpret_cast<uintptr_t>(out + sh.head) ^ reinterpret_cast<uintptr_t>(sh.row + sh.head)) & 15u) == 0) {
                     uint4* out_vec = reinterpret_cast<uint4*>(out + sh.head) + sh.v0 + tid;
@@ -1299,7 +1308,7 @@ extern "C" bcq_status bcq_distill_loss(int n, int vocab, int k, const void* logi
     DistillParams p;
     p.n = n; p.vocab = vocab; p.k = k; p.tail = tail != 0; p.ld = (long long)ld; p.ldd = 0;
     p.index = top_index; p.logp = top_logprob; p.dloss = nullptr;
-    p.c = exponent_scale(temperature); p.inv_t = 1.0f / temperature; p.inv_t64 = 1.0 / (double)temperature;
+    p.c = exponent_scale(temperature); p.inv_t = 1.0f / temperature;
     p.loss = loss;
     cudaStream_t s = (cudaStream_t)stream;
     return dtype == BCQ_BF16 ? launch_distill<__nv_bfloat16, false>(n, logits, nullptr, p, s)
@@ -1320,7 +1329,7 @@ extern "C" bcq_status bcq_distill_grad(int n, int vocab, int k, const void* logi
     DistillParams p;
     p.n = n; p.vocab = vocab; p.k = k; p.tail = tail != 0; p.ld = (long long)ld; p.ldd = (long long)lddl;
     p.index = top_index; p.logp = top_logprob; p.dloss = dloss;
-    p.c = exponent_scale(temperature); p.inv_t = 1.0f / temperature; p.inv_t64 = 1.0 / (double)temperature;
+    p.c = exponent_scale(temperature); p.inv_t = 1.0f / temperature;
     p.loss = loss;
     cudaStream_t s = (cudaStream_t)stream;
     return dtype == BCQ_BF16 ? launch_distill<__nv_bfloat16, true>(n, logits, dlogits, p, s) : launch_distill<float, true>(n, logits, dlogits, p, s);

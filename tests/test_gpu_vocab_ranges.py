@@ -14,6 +14,7 @@ from test_gpu_vocab import check_logprobs, close, eps_s, make_logits, ref_distil
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
+INF = math.inf
 BF16, F32 = torch.bfloat16, torch.float32
 
 
@@ -28,6 +29,17 @@ def check_distill(x, index, logp, T, tail, w=None):
     n, vocab = x.shape
     w = torch.linspace(-1.0, 2.0, n, device="cuda") if w is None else w
     ref, grad, size = ref_distill(x, index, logp, T, tail)
+    if tail:
+        # the shares of the tokens outside the list in their sum, relative to its own largest (next to 1e20 the logarithm of a sum of many is nothing, in
+        # 64 bits too)
+        named = torch.zeros(x.shape, device="cuda").scatter_add_(1, index.long().clamp(min=0), (index >= 0).float()) > 0
+        rest = torch.where(named, -INF, x.double())
+        share = torch.nan_to_num(torch.softmax((rest - rest.amax(dim=1, keepdim=True)) / T, dim=1))
+        lq = torch.log_softmax((x.double() - x.double().amax(dim=1, keepdim=True)) / T, dim=1)
+        t = torch.zeros_like(lq).scatter_add_(1, index.long().clamp(min=0), torch.where(index >= 0, torch.exp(logp.double()), 0.0))
+        mass = t.sum(dim=1, keepdim=True)
+        r = torch.where(share.sum(dim=1, keepdim=True) > 0, (1.0 - mass).clamp(min=0.0), 0.0)
+        grad, size = (torch.exp(lq) * (mass + r) - t - share * r) / T, (torch.exp(lq) * (mass + r) + t + share * r) / T
     e = eps_s(vocab)
     tol = 2 * e + 2.0 ** -22 * ref.abs().clamp(max=1e30)
     loss = bcq.distill_loss(x, index, logp, T, tail)
@@ -38,6 +50,61 @@ def check_distill(x, index, logp, T, tail, w=None):
     half = torch.finfo(x.dtype).eps / 2
     close(d, grad * wd, (2 * e + 2.0 ** -20) * size * wd.abs() + half * (grad * wd).abs() * 1.01 + 2.0 ** -125 * (wd.abs() / T).clamp(min=1.0))
     return loss, d
+
+
+FINITE_MASKS = [-7.2e5, -1e9, -1e10, -1e12, -1e20]
+
+
+def place(x, index, value, keep=()):
+    """x with `value` in all columns but those of index and of keep."""
+    cols = torch.cat([index.long()] + [torch.full_like(index[:, :1], j).long() for j in keep], dim=1)
+    return torch.full_like(x, value).scatter(1, cols, x.gather(1, cols))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T", [0.296875, 0.5, 1.0, 2.0])
+@pytest.mark.parametrize("mask", FINITE_MASKS)
+def test_logprobs_finite_masks_of_any_size(dtype, T, mask):
+    for n, vocab in ((3, 50257), (600, 5003)):
+        x = make_logits(n, vocab, dtype, seed=3)
+        _, index = x.float().topk(12, dim=1)
+        targets = index[:, 5].contiguous()
+        check_logprobs(place(x, index, mask), targets, 20, T)          # most columns: most threads see nothing else
+        check_logprobs(place(x, index[:, 5:6], mask), targets, 0, T)
+        check_logprobs(torch.full_like(x, mask), targets, 5, T)        # the whole row
+        check_logprobs(torch.full_like(x, -mask), targets, 5, T)
+        check_logprobs(place(x, index, -mask), targets, 5, T)
+        check_logprobs((x.float() + mask).to(dtype), targets, 5, T)
+        check_logprobs((x.float() - mask).to(dtype), targets, 5, T)
+
+
+@pytest.mark.parametrize("T", [1.0, 1 / 512, 512.0])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_large_logits_on_both_sides_of_a_line(T, sign):
+    # rows whose elements lie on both sides of |x| log2(e) / T = 2^k: threads whose maxima are on different sides meet
+    for lg in (10, 16, 20, 24):
+        at = sign * 2.0 ** lg * math.log(2.0) * T
+        for n, vocab in ((2, 20001), (350, 3001)):
+            x = (make_logits(n, vocab, F32, seed=lg) * T + at).contiguous()
+            check_logprobs(x, torch.arange(n, device="cuda"), 10, T)
+            index, logp = teacher_of(make_logits(n, vocab, F32, seed=lg), 10, 1.0)
+            for tail in (True, False):
+                check_distill(x, index, logp, T, tail)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("tail", [True, False])
+@pytest.mark.parametrize("mask", FINITE_MASKS)
+def test_distill_finite_masks_of_any_size(dtype, tail, mask):
+    for n, vocab, T in ((3, 50257, 1.0), (500, 5003, 0.296875), (40, 5003, 2.0)):
+        x = make_logits(n, vocab, dtype, seed=4)
+        index, logp = teacher_of(x, 16, T)
+        for y in (place(x, index, mask), place(x, index, mask, keep=(0, vocab - 1)), place(x, index[:, :1], mask), torch.full_like(x, mask),
+                  torch.full_like(x, -mask), (x.float() + mask).to(dtype), (x.float() - mask).to(dtype)):
+            check_distill(y, index, logp, T, tail)
+        # what the teacher leaves to all others is next to nothing
+        sharp = torch.log_softmax(logp, dim=1) - 1e-7
+        check_distill(place(x, index, mask), index, sharp, T, tail)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
