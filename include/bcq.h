@@ -313,7 +313,7 @@ bcq_status bcq_token_logprobs(int n, int vocab, const void* logits, size_t ld, i
  * top_index int32 [n][k], top_logprob float [n][k], 1 <= k <= 128, p = exp(top_logprob); entries with a negative index are
  * left out, one >= vocab makes the row's results NaN, an index that is there twice has the sum of its p.  q is the
  * student's distribution, softmax(x / temperature).
- *   tail = 0: p is normalised to 1 (a row without entries has loss 0);
+ *   tail = 0: p is normalised to 1, however small it is (a row without entries has loss 0);
  *             loss = sum_i p_i (log p_i - log q_i).  k = 1 and a log probability of 0: cross entropy with a label
  *   tail = 1: all other tokens are one class, with r = max(0, 1 - sum p) at the teacher and rho at the student;
  *             loss = sum_i p_i (log p_i - log q_i) + r (log r - log rho).  Where there is no other token above -inf, r counts as 0

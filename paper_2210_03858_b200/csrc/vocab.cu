@@ -747,11 +747,12 @@ struct Teacher {
     int index[kTopMax];   // -1: left out
     float logp[kTopMax];
     float x[kTopMax];     // the student's logit of the token
-    double p[kTopMax];
+    double p[kTopMax];    // relative to the likeliest entry's without a tail
     int word[kTopMax];       // of its mark; -1: not in this CTA's share
     float mass_of[kTopMax];  // p of all entries with this index, normalised without a tail; in the first of them
     int first[kTopMax];      // 1: the first entry with this index
     double total;            // of p
+    float log_base;          // logarithm of what p is relative to
     float own_m, own_s;      // largest logit of these tokens, and their sum relative to it
     float mass, r;           // of the teacher's tokens (1 without a tail), of all others
     float w;                 // what the row counts
@@ -845,6 +846,16 @@ __device__ __forceinline__ void prepare_row(const DistillParams& p, const Share<
                 }
         }
     }
+    // without a tail only ratios of probabilities count, and these may be too small for 64 bits: they are taken relative to the largest
+    float log_base = 0.0f;
+    if (!p.tail) {
+        float most = neg_inf();
+#pragma unroll
+        for (int u = 0; u < kTopMax / 32; ++u)
+            if (index[u] >= 0) most = fmaxf(most, logp[u]);
+        most = value_of(__reduce_max_sync(0xffffffffu, order_of(most)));
+        if (most > neg_inf()) log_base = most;
+    }
     double total = 0.0;
 #pragma unroll
     for (int u = 0; u < kTopMax / 32; ++u) {
@@ -853,7 +864,7 @@ __device__ __forceinline__ void prepare_row(const DistillParams& p, const Share<
         te->index[i] = index[u];
         te->logp[i] = logp[u];
         te->x[i] = x[u];
-        const double q = index[u] >= 0 ? exp((double)logp[u]) : 0.0;
+        const double q = index[u] >= 0 ? exp((double)logp[u] - (double)log_base) : 0.0;
         te->p[i] = q;
         total += q;
         if (!(x[u] < __int_as_float(0x7f800000))) bad = true;
@@ -886,6 +897,7 @@ __device__ __forceinline__ void prepare_row(const DistillParams& p, const Share<
     bad = __any_sync(0xffffffffu, bad);
     if (lane == 0) {
         te->total = total;
+        te->log_base = log_base;
         te->own_m = m;
         te->own_s = s;
         const double mass = p.tail ? total : (total == 0.0 ? 0.0 : total * keep);
@@ -928,7 +940,7 @@ __device__ __forceinline__ float loss_of_row(const DistillParams& p, const Teach
     for (int i = lane; i < p.k; i += 32) {
         if (te->index[i] < 0) continue;
         const double log_q = log_rel(te->x[i], base, p.c) - log_s;
-        loss += class_loss(te->p[i] * keep, (double)te->logp[i] + log_keep, log_q);
+        loss += class_loss(te->p[i] * keep, ((double)te->logp[i] - (double)te->log_base) + log_keep, log_q);
         if (!te->first[i]) loss -= exp(log_q);  // its q counts once
     }
     loss = warp_sum(loss);

@@ -155,3 +155,23 @@ def test_loss_of_tokens_that_the_teacher_all_but_excludes(dtype, tail):
         low = logp.clone()
         low[:, :4] = torch.tensor(values, device="cuda")    # the student's likeliest
         check_distill(x, index, low, 1.0, tail)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_probabilities_are_normalised_however_small_they_are(dtype):
+    # without a tail a constant added to a list's log probabilities changes nothing; multiples of 2^-10, so that it is added exactly
+    x = make_logits(60, 2003, dtype, seed=22)
+    index, logp = teacher_of(x, 9, 1.0)
+    logp = torch.round(logp * 1024.0) / 1024.0
+    index[5, 1:] = -1
+    logp[6, 3:] = -INF
+    w = torch.linspace(-1.0, 2.0, 60, device="cuda")
+    loss, d = check_distill(x, index, logp, 1.0, False, w)
+    for shift in (-690.0, -705.0, -735.0, -800.0, -2000.0, 500.0, 1000.0):
+        got, grad = bcq.distill_grad(x, index, logp + shift, w, 1.0, False)
+        assert torch.equal(got, bcq.distill_grad(x, index, logp, w, 1.0, False)[0]) and torch.equal(grad, d), shift
+        assert torch.equal(bcq.distill_loss(x, index, logp + shift, 1.0, False), loss), shift
+    # a list that gives nothing to any of its tokens is none
+    logp[:] = -INF
+    loss, d = bcq.distill_grad(x, index, logp, w, 1.0, False)
+    assert not loss.any() and not d.any()
