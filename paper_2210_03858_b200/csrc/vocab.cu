@@ -1061,13 +1061,13 @@ __device__ __noinline__ void rest_of_row(const Share<T> sh, T* out, float m, flo
 
 constexpr int kDistillThreads = 256;  // that go through a row; one more warp helps them
 
-// Loss, and with GRAD the gradient.  A CTA (or a cluster of them) goes from row to row, as far as the grid leaves it several.  Eight
-// warps go through the logits: once for the sums, and for the gradient once more, backwards, which finds the end of the row in L1 and
-// most of the rest in L2 (2048 rows of 50257, bf16: 109 us forwards and past L1, 97 so).  A ninth
-// is a row ahead of them with the teacher's list, whose loads depend on one another, and a row behind with the loss,
-// which is a chain of logarithms in 64 bits; so neither holds up the loads, of which two batches a thread are always on
-// their way.  Barriers: `ready` when a row's tokens are marked, `listed` when the rest of its list is there, `done` when its sums
-// are and its list is no longer read; each for odd and for even rows.
+// Loss, and with GRAD the gradient.  A CTA (or a cluster of them) goes from row to row for the loss, as far as the grid leaves it
+// several, and has one row for the gradient (the grid has a cluster for each).  Eight warps go through the logits: once for the sums, and for the gradient once more,
+// backwards, which finds the end of the row in L1 and most of the rest in L2 (2048 rows of 50257, bf16: 109 us forwards and past L1,
+// 97 so).  A ninth has the teacher's list, whose loads depend on one another, and the loss, which is a chain of logarithms in 64 bits:
+// a row ahead of the others and a row behind where there are several, so neither holds up the loads, of which two batches a thread are
+// always on their way.  Barriers: `ready` when a row's tokens are marked, `listed` when the rest of its list is there, `done` when its
+// sums are and its list is no longer read; each for odd and for even rows.
 // The gradient of 2048 rows of 50257, bf16: 94 us; with the row kept in shared memory 139 (a CTA a row, two CTAs an SM), 119 (one CTA an SM that writes a row's gradient while it takes the next one's sums, through
 // registers) and 127 (the same by bulk copies).  One CTA an SM has too few warps for the fixed part of a row, and
 // what the SM's L2 traffic saves comes back as waits.
@@ -1078,12 +1078,13 @@ distill_kernel(const T* logits, T* grad, const DistillParams p) {
     constexpr uint32_t kReady = 2, kListed = 4, kDone = 6;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ Stats part[NT / 32];
-    __shared__ Stats mine[2];
-    __shared__ Teacher teachers[2];
+    constexpr int kSlots = GRAD ? 1 : 2;  // rows that are in hand at a time
+    __shared__ Stats mine[kSlots];
+    __shared__ Teacher teachers[kSlots];
     const int tid = (int)threadIdx.x, rank = (int)blockIdx.x & (p.ctas - 1);
     const int step = (int)gridDim.x >> p.lg;
     uint32_t* marks = reinterpret_cast<uint32_t*>(smem);
-    for (int i = tid; i < p.marks_bytes / 2; i += NT + 32) marks[i] = 0;
+    for (int i = tid; i < kSlots * p.marks_bytes / 4; i += NT + 32) marks[i] = 0;
     __syncthreads();
     pdl_wait();
     auto share = [&](int row) { return Share<T>(logits + (long long)row * p.ld, p.vocab, rank, p.lg); };
@@ -1092,15 +1093,17 @@ distill_kernel(const T* logits, T* grad, const DistillParams p) {
     if (tid >= NT) {
         int it = 0;
         for (;; row += step, ++it) {
-            if (row < p.n) {
-                prepare_row<T>(p, share(row), row, &teachers[it & 1], marks + (it & 1) * (p.marks_bytes / 4), it >= 2, [&] {
+            const bool there = GRAD ? it == 0 : row < p.n;
+            const int slot = it & (kSlots - 1);
+            if (there) {
+                prepare_row<T>(p, share(row), row, &teachers[slot], marks + slot * (p.marks_bytes / 4), it >= 2, [&] {
                     __syncwarp();
-                    asm volatile("bar.arrive %0, %1;" ::"r"(kReady + (it & 1)), "n"(NT + 32) : "memory");
+                    asm volatile("bar.arrive %0, %1;" ::"r"(kReady + slot), "n"(NT + 32) : "memory");
                 });
-                asm volatile("bar.arrive %0, %1;" ::"r"(kListed + (it & 1)), "n"(NT + 32) : "memory");
+                asm volatile("bar.arrive %0, %1;" ::"r"(kListed + slot), "n"(NT + 32) : "memory");
             }
             if (it > 0) {
-                const int last = (it - 1) & 1;
+                const int last = (it - 1) & (kSlots - 1);
                 ptx::named_bar_sync(kDone + last, NT + 32);
                 if (rank == 0 && p.loss != nullptr) {
                     const float loss = loss_of_row(p, &teachers[last]);
@@ -1108,19 +1111,21 @@ distill_kernel(const T* logits, T* grad, const DistillParams p) {
                 }
                 __syncwarp();
             }
-            if (row >= p.n) break;
+            if (!there) break;
             if (p.ctas > 1) ptx::cluster_sync();  // (that of join_row)
         }
-    } else if (row < p.n) {
+    } else {
         uint4 va[kBatch], vb[kBatch];
         Stream<T, NT, GRAD>(share(row)).start(va, vb);
+        // (one turn for the gradient; with that said here the compiler's order of instructions costs fp32 6 %, 176 us and not 166)
         for (int it = 0; row < p.n; row += step, ++it) {
+            const int slot = it & (kSlots - 1);
             const Share<T> sh = share(row);
             const Stream<T, NT, GRAD> stream(sh);
             const float single = sh.single >= 0 ? Elem<T>::get(sh.row + sh.single) : 0.0f;
-            Teacher* te = &teachers[it & 1];
-            const uint8_t* mark = reinterpret_cast<const uint8_t*>(marks) + (it & 1) * p.marks_bytes;
-            ptx::named_bar_sync(kReady + (it & 1), NT + 32);
+            Teacher* te = &teachers[slot];
+            const uint8_t* mark = reinterpret_cast<const uint8_t*>(marks) + slot * p.marks_bytes;
+            ptx::named_bar_sync(kReady + slot, NT + 32);
             Running<T, false> run;
             stream.run(va, vb, [&](auto whole, int b, uint4(&v)[kBatch], int have) {
                 const int at = b * (kBatch * NT) + tid + 1;
@@ -1139,11 +1144,10 @@ distill_kernel(const T* logits, T* grad, const DistillParams p) {
                 if (!((mark[at / E] >> (at % E)) & 1)) run.one(single, p.c);
             }
             // what comes next is on its way while the sums are joined: the row again, or the next one
-            const int next = row + step;
             if (GRAD) stream.start_back(va, vb);
-            else if (next < p.n) Stream<T, NT>(share(next)).start(va, vb);
-            const Stats rest = join_row<NT>(run, part, &mine[it & 1], p.ctas, p.c);
-            ptx::named_bar_sync(kListed + (it & 1), NT + 32);
+            else if (row + step < p.n) Stream<T, NT>(share(row + step)).start(va, vb);
+            const Stats rest = join_row<NT>(run, part, &mine[slot], p.ctas, p.c);
+            ptx::named_bar_sync(kListed + slot, NT + 32);
             const float own_m = te->own_m, m = fmaxf(rest.m, own_m), base = m == neg_inf() ? 0.0f : m;
             const float down = ex2(fmaxf(rel_base(rest.m, base, p.c), kFloor));
             const float s = te->own_s * ex2(fmaxf(rel_base(own_m, base, p.c), kFloor)) + rest.s * down;
@@ -1204,14 +1208,13 @@ distill_kernel(const T* logits, T* grad, const DistillParams p) {
                     for (int j = sh.first + tid; j < min(lo, sh.last); j += NT) out[j] = from_float<T>(g(Elem<T>::get(sh.row + j)));
                     for (int j = hi + tid; count > 0 && j < sh.last; j += NT) out[j] = from_float<T>(g(Elem<T>::get(sh.row + j)));
                 }
-                if (next < p.n) Stream<T, NT, GRAD>(share(next)).start(va, vb);
                 row_sync<NT>();
                 if (tid < p.k && te->first[tid] && te->index[tid] >= sh.first && te->index[tid] < sh.last) {
                     const float q = ex2(rel(te->x[tid], base, p.c)) * f_own;
                     out[te->index[tid]] = from_float<T>(zero ? 0.0f : q - te->mass_of[tid] * f);
                 }
             }
-            asm volatile("bar.arrive %0, %1;" ::"r"(kDone + (it & 1)), "n"(NT + 32) : "memory");
+            asm volatile("bar.arrive %0, %1;" ::"r"(kDone + slot), "n"(NT + 32) : "memory");
         }
     }
     __syncwarp();
@@ -1268,7 +1271,7 @@ bcq_status launch_distill(int n, const void* logits, void* grad, DistillParams p
     p.ctas = ctas_for(n, p.vocab, (int)sizeof(T), kDistillThreads, 3);
     p.lg = log2_of(p.ctas);
     p.marks_bytes = (int)align_up((size_t)max_vectors(p.vocab, (int)sizeof(T), p.ctas) + 2, 16);
-    const size_t smem = 2 * (size_t)p.marks_bytes;
+    const size_t smem = (GRAD ? 1 : 2) * (size_t)p.marks_bytes;
     const bcq_status st = ensure_dynamic_smem(distill_kernel<T, GRAD>, smem);
     if (st != BCQ_OK) return st;
     // The loss goes from row to row (2048 rows of 50272, fp32: 69 us, a CTA for each 74); the gradient, whose rows take longer than a CTA's
