@@ -5,7 +5,7 @@
 // for its sums (and the gradient's once more, from L2 as far as it is still there): a thread keeps a running maximum and the sums that go with it, and rescales them when a batch of its
 // vectors has a larger one, so no second pass is needed for the sums; the sums of threads, warps and CTAs are joined in
 // a fixed order.  b is the rounded product and is subtracted everywhere (from a target, from an alternative), so its
-// rounding error, which would be that of a probability, drops out (where it would be too large for that, |b| > 2^20, exponents
+// rounding error, which would be that of a probability, drops out (where it would be too large for that, |b| > 2^31, exponents
 // are c (x - max x)).  What bounds them is memory: n vocab sizeof(T) bytes read (and written, for the gradient).  Next to that is the issue of instructions: an element of bf16 costs a
 // conversion, an exponential (16 a cycle and SM: 0.7 of the time its bytes take), half a product and half a sum for each
 // result (two at a time, fma.rn.f32x2), a quarter of a maximum and half a clamp, and with everything that goes with a row
@@ -83,9 +83,11 @@ __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
 }
 
 // The base of a sum with maximum m is the rounded product b = rn(m c) where it is at most this either way, and m c itself beyond, with
-// exponents (x - m) c.  Subtracting b from c x leaves b's rounding error in the exponent, 2^-5 at most: the same for all terms, so it
-// drops out; of a product of 1e10 it would be hundreds, and the sum infinite or 0.
-constexpr float kNear = 1048576.0f;  // 2^20
+// exponents (x - m) c.  Subtracting b from c x leaves b's rounding error in the exponent, half a step of b: 2^6 at most, the same for
+// all terms, so it drops out (sums are below 2^90 with it, and a logit next to m is a step of m away, so the exponents lose nothing).  Of
+// a product of 1e10 it would be hundreds, and the sum infinite or 0.  (2^31 and not less, since masks of -1e9 are common: threads that
+// see nothing else take 1.2 to 1.7 times as long with the other kind of base.)
+constexpr float kNear = 2147483648.0f;
 // Logits below this are as good as this one next to a base that is near, and times c it is finite.
 constexpr float kLowest = -1.26765060e30f;  // -2^100
 
@@ -957,44 +959,51 @@ __device__ __forceinline__ float from_float<float>(float x) { return x; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
-// The gradient of a token that the teacher does not name, f 2^(c x - b).  In bf16 the magnitude of f is part of the exponent, which
-// saves a product: the sign is left.  The sum log2|f| - b is rounded, so this is done only where it is below 2^10: the result is off by
-// 2^-15 of itself then, a hundredth of half a step (and by the error of the logarithm, 2^-18).  fits() says whether it is; a row
-// where it is not (c max x beyond 1000 or so) goes to rest_of_row().
-template <typename T>
+// The gradient of a token that the teacher does not name, f 2^(c (x - m)).  FOLDED: the magnitude of f is part of the exponent, which
+// saves a product and a sum, and the sign is left.  The sum log2|f| - c m is rounded, so this is for bf16 and sums below 2^10: the result
+// is off by 2^-15 of itself then, a hundredth of half a step (and by the error of the logarithm, 2^-18).
+template <typename T, bool FOLDED>
 struct RestGrad {
-    float c, nb, f;  // bf16: f is 1 or -1
+    float c, from, f;  // FOLDED: log2|f| - c m, and 1 or -1
 
-    __device__ __forceinline__ RestGrad() {}
-    __device__ __forceinline__ RestGrad(float f_, float c_, float b) : c(c_), nb(-b), f(f_) {
-        if (sizeof(T) == 2) {
-            nb += log2f(fabsf(f));
+    __device__ __forceinline__ RestGrad(float f_, float m, float c_) : c(c_), from(-m), f(f_) {
+        if (FOLDED) {
+            const float b = __fmul_rn(m, c);
+            from = (log2f(fabsf(f)) - fmaf(m, c, -b)) - b;
             f = f < 0.0f ? -1.0f : 1.0f;
         }
     }
-    // (-inf: all are zero; NaN: all are)
-    __device__ __forceinline__ bool fits() const { return sizeof(T) == 4 || !(fabsf(nb) > 1024.0f) || nb == neg_inf(); }
-    __device__ __forceinline__ float operator()(float x) const { return ex2(fmaf(x, c, nb)) * f; }
+    // (-inf: all results are zero)
+    __device__ __forceinline__ bool fits() const { return fabsf(from) <= 1024.0f || from == neg_inf(); }
+    __device__ __forceinline__ f32x2 exponents(f32x2 x) const {
+        const f32x2 c2 = pack2(c, c), from2 = pack2(from, from);
+        return FOLDED ? fma2(x, c2, from2) : mul2(add2(x, from2), c2);
+    }
+    __device__ __forceinline__ T operator()(float x) const {
+        float a, b;
+        unpack2(exponents(pack2(x, x)), a, b);
+        return from_float<T>(ex2(a) * f);
+    }
     // of a vector
     __device__ __forceinline__ uint4 operator()(const uint4& x) const {
         constexpr int E = Elem<T>::E;
-        const f32x2 c2 = pack2(c, c), nb2 = pack2(nb, nb), f2 = pack2(f, f);
+        const f32x2 f2 = pack2(f, f);
         const uint32_t sign = f < 0.0f ? 0x80008000u : 0u;
         uint32_t y[4];
 #pragma unroll
         for (int i = 0; i < E; i += 2) {
             float a, b;
-            unpack2(fma2(pack2(Elem<T>::at(x, i), Elem<T>::at(x, i + 1)), c2, nb2), a, b);
+            unpack2(exponents(pack2(Elem<T>::at(x, i), Elem<T>::at(x, i + 1))), a, b);
             a = ex2(a);
             b = ex2(b);
+            if (!FOLDED) unpack2(mul2(pack2(a, b), f2), a, b);
             if constexpr (sizeof(T) == 4) {
-                unpack2(mul2(pack2(a, b), f2), a, b);
                 y[i] = __float_as_uint(a);
                 y[i + 1] = __float_as_uint(b);
             } else {
                 const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
                 memcpy(&y[i / 2], &h, 4);
-                y[i / 2] ^= sign;
+                if (FOLDED) y[i / 2] ^= sign;
             }
         }
         return make_uint4(y[0], y[1], y[2], y[3]);
@@ -1035,28 +1044,6 @@ __device__ __forceinline__ void zero_row(T* out, int first, int last, int tid, i
     for (int v = tid; v < count; v += threads) st_stream(reinterpret_cast<uint4*>(out + from) + v, make_uint4(0u, 0u, 0u, 0u));
     if (tid < before) out[first + tid] = from_float<T>(0.0f);
     if (tid < last - after) out[after + tid] = from_float<T>(0.0f);
-}
-
-// The gradient of the tokens that the teacher does not name, all of this CTA's share, where RestGrad does not do: f 2^rel(x, m), element
-// by element, in whole vectors where logits and result have them at the same places.
-template <typename T>
-__device__ __noinline__ void rest_of_row(const Share<T> sh, T* out, float m, float f, float c, int tid, int threads) {
-    constexpr int E = Elem<T>::E;
-    auto grad = [&](float x) { return from_float<T>(ex2(rel(x, m, c)) * f); };
-    if (((reinterpret_cast<uintptr_t>(out + sh.head) ^ reinterpret_cast<uintptr_t>(sh.row + sh.head)) & 15u) == 0) {
-        for (int v = sh.v0 + tid; v < sh.v1; v += threads) {
-            const uint4 x = ld(sh.vec(v));
-            T y[E];
-#pragma unroll
-            for (int i = 0; i < E; ++i) y[i] = grad(Elem<T>::at(x, i));
-            uint4 w;
-            memcpy(&w, y, 16);
-            st_stream(reinterpret_cast<uint4*>(out + sh.head) + v, w);
-        }
-        if (sh.single >= 0) out[sh.single] = grad(Elem<T>::get(sh.row + sh.single));
-    } else {
-        for (int j = sh.first + tid; j < sh.last; j += threads) out[j] = grad(Elem<T>::get(sh.row + j));
-    }
 }
 
 constexpr int kDistillThreads = 256;  // that go through a row; one more warp helps them
@@ -1117,7 +1104,7 @@ distill_kernel(const T* logits, T* grad, const DistillParams p) {
     } else {
         uint4 va[kBatch], vb[kBatch];
         Stream<T, NT, GRAD>(share(row)).start(va, vb);
-        // (one turn for the gradient; with that said here the compiler's order of instructions costs fp32 6 %, 176 us and not 166)
+        // (one turn for the gradient; said here, that makes for an order of instructions that costs fp32 6 %, 176 us and not 166)
         for (int it = 0; row < p.n; row += step, ++it) {
             const int slot = it & (kSlots - 1);
             const Share<T> sh = share(row);
@@ -1167,50 +1154,57 @@ distill_kernel(const T* logits, T* grad, const DistillParams p) {
                 const float w = te->w;
                 const bool zero = w == 0.0f;
                 const float r = rest.s > 0.0f ? te->r : 0.0f, f = w * p.inv_t, mass = te->mass + r;
-                const float f_rest = none ? quiet_nan() : f * (mass * (down / s) - (r > 0.0f ? r / rest.s : 0.0f));
-                const float b_rest = __fmul_rn(m_rest, p.c);
-                const RestGrad<T> g(f_rest, p.c, b_rest);
-                const float f_own = none ? quiet_nan() : f * mass / s;
+                // Sums relative to c times their maxima, without the rounding of their bases: a small result would be 0 with it.
+                const float to_base = ex2(base_error(base, p.c)) / s, r_share = r > 0.0f ? r / rest.s * ex2(base_error(m_rest, p.c)) : 0.0f;
+                const float f_rest = none ? quiet_nan() : f * (mass * (ex2((rest.m - base) * p.c) * to_base) - r_share);
+                const float f_own = none ? quiet_nan() : f * mass * to_base;
                 T* out = grad + (long long)row * p.ldd;
+                auto others = [&](const auto& g) {
+                    if (((reinterpret_cast<uintptr_t>(out + sh.head) ^ reinterpret_cast<uintptr_t>(sh.row + sh.head)) & 15u) == 0) {
+                        uint4* out_vec = reinterpret_cast<uint4*>(out + sh.head) + sh.v0 + tid;
+                        stream.run_back(va, vb, [&](auto whole, int b, uint4(&v)[kBatch], int have) {
+#pragma unroll
+                            for (int u = 0; u < kBatch; ++u)
+                                if (decltype(whole)::value || u < have) st_stream(out_vec + b * (kBatch * NT) + u * NT, g(v[u]));
+                        });
+                        if (sh.single >= 0) out[sh.single] = g(single);
+                    } else {
+                        // The result's rows start elsewhere than the logits': its whole vectors, each from two of the logits',
+                        // where both are this CTA's; single elements for the rest.
+                        const int from = sh.head + sh.v0 * E;  // of the elements in whole vectors of logits
+                        const int before = (int)(((16u - (uint32_t)(reinterpret_cast<uintptr_t>(out + from) & 15u)) & 15u) / sizeof(T));
+                        const int count = max(0, sh.v1 - sh.v0 - 1);
+                        uint4* out_vec = reinterpret_cast<uint4*>(out + from + before);
+                        for (int v = (count - 1) / (kBatch * NT) * (kBatch * NT) + tid; v >= 0; v -= kBatch * NT) {
+                            const uint4* at = sh.vec(sh.v0 + v);  // (a neighbour's vector is in L1 by then, or on its way)
+#pragma unroll
+                            for (int u = 0; u < kBatch; ++u)
+                                if (v + u * NT < count) {
+                                    va[u] = ld(at + u * NT);
+                                    vb[u] = ld(at + u * NT + 1);
+                                }
+#pragma unroll
+                            for (int u = 0; u < kBatch; ++u)
+                                if (v + u * NT < count) st_stream(out_vec + v + u * NT, g(shifted<T>(va[u], vb[u], before)));
+                        }
+                        const int lo = count > 0 ? from + before : sh.last, hi = from + before + count * E;
+                        for (int j = sh.first + tid; j < min(lo, sh.last); j += NT) out[j] = g(Elem<T>::get(sh.row + j));
+                        for (int j = hi + tid; count > 0 && j < sh.last; j += NT) out[j] = g(Elem<T>::get(sh.row + j));
+                    }
+                };
                 // (the teacher's tokens, whose exponent may overflow here, are written after the others)
                 if (zero) {
                     zero_row(out, sh.first, sh.last, tid, NT);
-                } else if (!is_near(b_rest) || !g.fits()) {
-                    rest_of_row<T>(sh, out, m_rest, f_rest, p.c, tid, NT);
-                } else if (((reinterpret_cast<uintptr_t>(out + sh.head) ^ reinterpret_cast<uintptr_t>(sh.row + sh.head)) & 15u) == 0) {
-                    uint4* out_vec = reinterpret_cast<uint4*>(out + sh.head) + sh.v0 + tid;
-                    stream.run_back(va, vb, [&](auto whole, int b, uint4(&v)[kBatch], int have) {
-#pragma unroll
-                        for (int u = 0; u < kBatch; ++u)
-                            if (decltype(whole)::value || u < have) st_stream(out_vec + b * (kBatch * NT) + u * NT, g(v[u]));
-                    });
-                    if (sh.single >= 0) out[sh.single] = from_float<T>(g(single));
+                } else if constexpr (sizeof(T) == 4) {
+                    others(RestGrad<T, false>(f_rest, m_rest, p.c));
                 } else {
-                    // The result's rows start elsewhere than the logits': its whole vectors, each from two of the logits',
-                    // where both are this CTA's; single elements for the rest.
-                    const int from = sh.head + sh.v0 * E;  // of the elements in whole vectors of logits
-                    const int before = (int)(((16u - (uint32_t)(reinterpret_cast<uintptr_t>(out + from) & 15u)) & 15u) / sizeof(T));
-                    const int count = max(0, sh.v1 - sh.v0 - 1);
-                    uint4* out_vec = reinterpret_cast<uint4*>(out + from + before);
-                    for (int v = (count - 1) / (kBatch * NT) * (kBatch * NT) + tid; v >= 0; v -= kBatch * NT) {
-                        const uint4* at = sh.vec(sh.v0 + v);  // (a neighbour's vector is in L1 by then, or on its way)
-#pragma unroll
-                        for (int u = 0; u < kBatch; ++u)
-                            if (v + u * NT < count) {
-                                va[u] = ld(at + u * NT);
-                                vb[u] = ld(at + u * NT + 1);
-                            }
-#pragma unroll
-                        for (int u = 0; u < kBatch; ++u)
-                            if (v + u * NT < count) st_stream(out_vec + v + u * NT, g(shifted<T>(va[u], vb[u], before)));
-                    }
-                    const int lo = count > 0 ? from + before : sh.last, hi = from + before + count * E;
-                    for (int j = sh.first + tid; j < min(lo, sh.last); j += NT) out[j] = from_float<T>(g(Elem<T>::get(sh.row + j)));
-                    for (int j = hi + tid; count > 0 && j < sh.last; j += NT) out[j] = from_float<T>(g(Elem<T>::get(sh.row + j)));
+                    const RestGrad<T, true> g(f_rest, m_rest, p.c);
+                    if (g.fits()) others(g);
+                    else others(RestGrad<T, false>(f_rest, m_rest, p.c));
                 }
                 row_sync<NT>();
                 if (tid < p.k && te->first[tid] && te->index[tid] >= sh.first && te->index[tid] < sh.last) {
-                    const float q = ex2(rel(te->x[tid], base, p.c)) * f_own;
+                    const float q = ex2((te->x[tid] - base) * p.c) * f_own;
                     out[te->index[tid]] = from_float<T>(zero ? 0.0f : q - te->mass_of[tid] * f);
                 }
             }

@@ -93,6 +93,24 @@ def test_large_logits_on_both_sides_of_a_line(T, sign):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("lg", [9, 10, 11, 29, 30, 31, 32, 40])
+def test_large_logits_some_steps_apart(dtype, sign, lg):
+    # |x| log2(e) / T around 2^lg, elements a few steps of their type from one another, and a few much further down
+    for n, vocab, T in ((2, 20001, 1.0), (350, 3001, 0.75), (5, 3001, 1 / 256)):
+        at = sign * 2.0 ** lg * math.log(2.0) * T
+        step = max(T, abs(at) * torch.finfo(dtype).eps)
+        x = (make_logits(n, vocab, F32, seed=lg) * step + at).to(dtype)
+        x[:, ::3] -= 30.0 * step
+        check_logprobs(x, torch.arange(n, device="cuda"), 10, T)
+        index, logp = teacher_of(make_logits(n, vocab, F32, seed=lg + 1), 10, 1.0)
+        _, likely = x.float().topk(10, dim=1)
+        for at_index in (index, likely.to(torch.int32)):
+            for tail in (True, False):
+                check_distill(x, at_index, logp, T, tail)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("tail", [True, False])
 @pytest.mark.parametrize("mask", FINITE_MASKS)
 def test_distill_finite_masks_of_any_size(dtype, tail, mask):
