@@ -149,11 +149,14 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const Rows r = rows_of(logits, "logits");
         const bool given = a[1] != Py_None;
         const at::Tensor* targets = given ? &dense(a[1], "targets", at::kLong, {r.n}) : nullptr;
-        const int top_k = (int)as_int(a[2]), k = std::max(0, top_k);
+        const int top_k = (int)as_int(a[2]);
         const float temperature = as_float(a[3]);
+        // (without rows it only looks at sizes: a list that is refused is not allocated)
+        const int fine = f_token_logprobs(0, r.cols, nullptr, r.ld, r.dtype, nullptr, top_k, temperature, nullptr, nullptr, nullptr, nullptr, nullptr);
+        if (fine != BCQ_OK) return PyLong_FromLong(fine);
         at::Tensor logprob;
         if (given) logprob = empty({r.n}, at::kFloat);
-        at::Tensor entropy = empty({r.n}, at::kFloat), top = empty({r.n, k}, at::kFloat), index = empty({r.n, k}, at::kInt);
+        at::Tensor entropy = empty({r.n}, at::kFloat), top = empty({r.n, top_k}, at::kFloat), index = empty({r.n, top_k}, at::kInt);
         const int st = without_gil([&] {
             return f_token_logprobs(r.n, r.cols, ptr(logits), r.ld, r.dtype, given ? ptr<const long long>(*targets) : nullptr, top_k, temperature,
                                     given ? ptr<float>(logprob) : nullptr, ptr<float>(entropy), ptr<float>(top), ptr<int>(index), stream());

@@ -193,3 +193,14 @@ def test_probabilities_are_normalised_however_small_they_are(dtype):
     logp[:] = -INF
     loss, d = bcq.distill_grad(x, index, logp, w, 1.0, False)
     assert not loss.any() and not d.any()
+
+
+def test_lists_that_are_refused_are_not_allocated():
+    x = make_logits(64, 100, F32)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.max_memory_allocated()
+    for k in (129, 10 ** 6, 2 ** 31 - 1):
+        with pytest.raises(bcq.BcqError):
+            bcq.token_logprobs(x, top_k=k)
+    assert torch.cuda.max_memory_allocated() - before <= 4096
