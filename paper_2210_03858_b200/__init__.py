@@ -472,11 +472,17 @@ def _ops():
     if _tensor_call is None:
         _torch()
         lib()
-        import importlib
+        import importlib.util
+        from .build import tensor_call_path
+        path = tensor_call_path()  # (that of the torch that is there)
+        if path is None or not os.path.exists(path):
+            raise RuntimeError("binding not built: run paper_2210_03858_b200/build.py")
+        spec = importlib.util.spec_from_file_location(__name__ + "._tensor_call", path)
         try:
-            mod = importlib.import_module(__name__ + "._tensor_call")
+            mod = importlib.util.module_from_spec(spec)
+            spec.loader.exec_module(mod)
         except ImportError as e:
-            raise RuntimeError("binding not built: run paper_2210_03858_b200/build.py (%s)" % e) from e
+            raise RuntimeError("binding cannot be loaded: run paper_2210_03858_b200/build.py --force (%s)" % e) from e
         mod.load(LIB_PATH)
         _tensor_call = mod
     return _tensor_call
