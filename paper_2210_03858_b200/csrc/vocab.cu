@@ -640,8 +640,10 @@ __device__ __forceinline__ float log_prob(float x, float m, float log_s, const L
 }
 
 // LIST 0: none; 1: a short one; 2: a long one, of which more batches are read again, so that the first reading leaves them in L1 as
-// far as there is room (4096 rows of 50257, bf16: 128 alternatives 136 us past L1 and 122 so, 64 110 and 103, 20 86 and 92).
-constexpr int kLongList = 32;
+// far as there is room.  Measured past L1 and so, us, for rows of 16000 to 131072 in bf16 and fp32, 1500 to 4096 of them: 20 alternatives
+// 47 to 237 and 52 to 247; 40 48 to 240 and 54 to 250 (past L1 is 1 to 16 % faster everywhere); 64 the one as often as the other (4096 rows of 50257
+// in bf16 110 and 103, 2048 of them 54 and 58; fp32 83 and 87); 96 60 to 99 and 62 to 92; 128 75 to 277 and 68 to 279.
+constexpr int kLongList = 48;
 template <typename T, int LIST>
 __global__ void __launch_bounds__(LIST ? kLpThreads : kLpThreadsPlain)
 token_logprobs_kernel(const T* logits, const LogprobParams p) {
