@@ -11,7 +11,10 @@ that a profiler can capture one or two launches of one kernel in a minute:
                         rounds (five 5120 x 5120 matrices), q = 4, g = 128
     logprobs [top]      1480 rows of 50257 bf16 logits, log probabilities and top alternatives (default 64)
     distill             1776 such rows, distillation loss and gradient against 64 alternatives of a teacher
+    loss [bf16]         888 rows of 50272 fp32 logits (bf16: 1776 of 50257 in bf16), the loss alone
     mx [n]              OPT-13B FFN up (5120 -> 20480) in microscaled 4-bit floating point, n tokens (default 2048)
+    mx_decode [n]       OPT-6.7B att_qkv (4096 -> 12288) in it, n tokens (default 1)
+    mx_quantize         16384 x 4096 fp32 values to it, and back to bf16
 """
 import sys
 
@@ -73,10 +76,10 @@ def _quantize(alt):
         bcq.quantize(W, 4, 128, alt)
 
 
-def _logits(n, seed):
+def _logits(n, seed, dtype=torch.bfloat16, vocab=50257):
     gen = torch.Generator(device="cuda")
     gen.manual_seed(seed)
-    return (torch.randn((n, 50304), generator=gen, device="cuda") * 2.0).bfloat16()[:, :50257]
+    return (torch.randn((n, 50304), generator=gen, device="cuda") * 2.0).to(dtype)[:, :vocab]
 
 
 def _logprobs(top):
@@ -93,13 +96,29 @@ def _distill():
         bcq.distill_grad(x, index, top, w)
 
 
-def _mx(n):
+def _loss(bf16):
+    n, dtype, vocab = (1776, torch.bfloat16, 50257) if bf16 else (888, torch.float32, 50272)
+    x = _logits(n, 1, dtype, vocab)
+    _, _, top, index = bcq.token_logprobs(_logits(n, 2, dtype, vocab), top_k=64)
+    for _ in range(3):
+        bcq.distill_loss(x, index, top)
+
+
+def _mx(n, d_in, d_out):
     gen = torch.Generator(device="cuda")
     gen.manual_seed(1)
-    W = bcq.mx_quantize(torch.randn((20480, 5120), generator=gen, device="cuda") * 0.02)
-    X = torch.randn((n, 5120), generator=gen, device="cuda").bfloat16()
+    W = bcq.mx_quantize(torch.randn((d_out, d_in), generator=gen, device="cuda") * 0.02)
+    X = torch.randn((n, d_in), generator=gen, device="cuda").bfloat16()
     for _ in range(3):
         bcq.mx_linear(X, W, out_dtype=torch.bfloat16)
+
+
+def _mx_quantize():
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    X = torch.randn((16384, 4096), generator=gen, device="cuda") * 0.02
+    for _ in range(3):
+        bcq.mx_dequantize(bcq.mx_quantize(X), out_dtype=torch.bfloat16)
 
 
 def main(argv):
@@ -114,8 +133,14 @@ def main(argv):
         _logprobs(int(argv[2]) if len(argv) > 2 else 64)
     elif case == "distill":
         _distill()
+    elif case == "loss":
+        _loss(len(argv) > 2 and argv[2] == "bf16")
     elif case == "mx":
-        _mx(int(argv[2]) if len(argv) > 2 else 2048)
+        _mx(int(argv[2]) if len(argv) > 2 else 2048, 5120, 20480)
+    elif case == "mx_decode":
+        _mx(int(argv[2]) if len(argv) > 2 else 1, 4096, 12288)
+    elif case == "mx_quantize":
+        _mx_quantize()
     else:
         raise SystemExit(__doc__)
     torch.cuda.synchronize()
