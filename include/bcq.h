@@ -264,7 +264,8 @@ bcq_status bcq_alpha_unpack(long long count, int nseg, const long long* seg_begi
 
 /* ------------------------------------------------------------------ microscaled 4-bit floating point
  *
- * The other 4-bit form of a matrix: what the tensor core multiplies as it is (the OCP microscaling format MXFP4).  Blocks of 32
+ * The other 4-bit form of a matrix: what the tensor core multiplies as it is (the OCP microscaling format MXFP4).  For matrices that are
+ * only multiplied from the left: there is no product with the transposed one (a dX).  Blocks of 32
  * consecutive elements of a row share a power of two, the last block of a row may be shorter; an element is a sign and one of
  * 0, 1/2, 1, 3/2, 2, 3, 4, 6 times it.  A matrix of `rows` x `cols` (at most 2^30 and 2^20) is held in two buffers, both 16-byte aligned:
  *   codes  : uint8 [rows][64 * ceil(cols / 128)], element k of a row in byte k / 2, even k in the low half; bit 3 is the sign, bits
@@ -276,7 +277,8 @@ bcq_status bcq_alpha_unpack(long long count, int nseg, const long long* seg_begi
 size_t bcq_mx_codes_bytes(int rows, int cols);
 size_t bcq_mx_scales_bytes(int rows, int cols);
 
-/* X [rows][ldx] (BCQ_F32 or BCQ_BF16, any alignment; rows that are 16-byte aligned are read faster) to codes and scales: a block's
+/* X [rows][ldx] (BCQ_F32 or BCQ_BF16, any alignment; read faster where X is aligned to 32 bytes (bf16: 16) and ldx is a multiple of 8) to
+ * codes and scales: a block's
  * exponent is floor(log2 max|x|) - 2, at least -127; x 2^-e goes to the nearest magnitude, ties to the even code, larger ones to 6.
  * A block that holds a NaN or an infinity gets the scale NaN.  rows = 0 is allowed. */
 bcq_status bcq_mx_quantize(int rows, int cols, const void* X, size_t ldx, int x_dtype, uint8_t* codes, uint8_t* scales, void* stream);
@@ -296,8 +298,9 @@ bcq_status bcq_mx_linear(int d_out, int d_in, int n, const uint8_t* x_codes, con
  * any element (no alignment beyond that of an element).  n = 0 is allowed and launches nothing; n <= 2^30, vocab <= 393216 and
  * lists of up to 128 tokens are covered (BCQ_ERR_UNSUPPORTED otherwise); 1e-3 <= temperature <= 1e3 (BCQ_ERR_SHAPE).
  * Logits of -inf are tokens that cannot occur.  A row that has a NaN or +inf, or nothing above -inf, is no
- * distribution: its results are NaN (indices -1).  Sums are kept in fp32 relative to the row's maximum and joined in a
- * fixed order, so a call gives the same result in every run. */
+ * distribution: its results are NaN (indices -1).  Logits of any finite size are covered.  Sums are kept in fp32 relative to the
+ * row's maximum and joined in a fixed order, so a call gives the same result in every run; a row's sum is within
+ * (vocab / 256 + 210) 2^-24 of itself. */
 
 /* Of every row x, with l = log sum_j exp(x_j / temperature):
  *   logprob     out: float [n], x[target] / temperature - l; 0 for a negative target (no token), NaN for one >= vocab.
@@ -311,7 +314,7 @@ bcq_status bcq_token_logprobs(int n, int vocab, const void* logits, size_t ld, i
 
 /* Distillation from a teacher's top log probabilities (as bcq_token_logprobs writes them at the same temperature):
  * top_index int32 [n][k], top_logprob float [n][k], 1 <= k <= 128, p = exp(top_logprob); entries with a negative index are
- * left out, one >= vocab makes the row's results NaN, an index that is there twice has the sum of its p.  q is the
+ * left out (so a teacher's row that was no distribution has no entries), one >= vocab makes the row's results NaN, an index that is there twice has the sum of its p.  q is the
  * student's distribution, softmax(x / temperature).
  *   tail = 0: p is normalised to 1, however small it is (a row without entries has loss 0);
  *             loss = sum_i p_i (log p_i - log q_i).  k = 1 and a log probability of 0: cross entropy with a label
@@ -321,7 +324,8 @@ bcq_status bcq_token_logprobs(int n, int vocab, const void* logits, size_t ld, i
 bcq_status bcq_distill_loss(int n, int vocab, int k, const void* logits, size_t ld, int dtype, const int* top_index,
                             const float* top_logprob, float temperature, int tail, float* loss, void* stream);
 
-/* The loss (may be NULL) and its gradient with respect to the logits, reading these once:
+/* The loss (may be NULL) and its gradient with respect to the logits, which are read twice, the second time from L1 and L2 as far as they are
+ * still there:
  *   dlogits[t][j] = dloss[t] d loss[t] / d x[t][j]   (d / dx of x / temperature included, no other factor)
  * dloss: float [n]; a row with dloss 0 gets zeros whatever its logits hold.  dlogits: dtype [n][lddl], lddl >= vocab; it may be
  * `logits` itself (then lddl = ld), but may not overlap it otherwise.  Elements behind a row's last are left as they are. */

@@ -555,7 +555,7 @@ def distill_loss(logits, top_index, top_logprob, temperature: float = 1.0, tail:
 
 def distill_grad(logits, top_index, top_logprob, dloss, temperature: float = 1.0, tail: bool = True, out=None):
     """bcq_distill_grad: as distill_loss, with dloss fp32 [n] (what the loss of each row counts) -> (loss fp32 [n], dlogits
-    [n][vocab] in the type of the logits).  ``out`` may be the logits themselves.  dlogits created here is a view whose rows are
+    [n][vocab] in the type of the logits).  ``out`` may be the logits themselves, and may not overlap them otherwise.  dlogits created here is a view whose rows are
     16-byte aligned, so a bf16 one is a dY for linear_bwd_x and linear_bwd_alpha."""
     return _done(_ops().distill_grad(logits, top_index, top_logprob, dloss, temperature, tail, out), "bcq_distill_grad")
 

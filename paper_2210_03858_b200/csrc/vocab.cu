@@ -11,8 +11,8 @@
 // result (two at a time, fma.rn.f32x2), a quarter of a maximum and half a clamp, and with everything that goes with a row
 // 7.6 instructions (9.1 with products and sums one at a time).
 // Measured: 2048 rows of 50304 in fp32, no list, 62 us, the rate of a copy; 4096 rows of 50257 in bf16, no list 66 us (95 %),
-// 64 alternatives 103; the loss of 2048 rows of 50272 in fp32 69 us (92 %), of 50257 in bf16 48 us (65 %), with the gradient 94 us
-// (67 %).
+// 64 alternatives 103; the loss of 2048 rows of 50272 in fp32 69 us (91 %), of 50257 in bf16 49 us (64 %), with the gradient 93 us
+// (68 %), in fp32 169 us (75 %).
 //
 // Rows start at any element (an odd vocabulary in bf16 leaves rows at odd addresses): the elements before the
 // first and after the last whole 16-byte vector of a row belong to single threads.
@@ -1057,7 +1057,7 @@ constexpr int kDistillThreads = 256;  // that go through a row; one more warp he
 // a row ahead of the others and a row behind where there are several, so neither holds up the loads, of which two batches a thread are
 // always on their way.  Barriers: `ready` when a row's tokens are marked, `listed` when the rest of its list is there, `done` when its
 // sums are and its list is no longer read; each for odd and for even rows.
-// The gradient of 2048 rows of 50257, bf16: 94 us; with the row kept in shared memory 139 (a CTA a row, two CTAs an SM), 119 (one CTA an SM that writes a row's gradient while it takes the next one's sums, through
+// The gradient of 2048 rows of 50257, bf16: 93 us; with the row kept in shared memory 139 (a CTA a row, two CTAs an SM), 119 (one CTA an SM that writes a row's gradient while it takes the next one's sums, through
 // registers) and 127 (the same by bulk copies).  One CTA an SM has too few warps for the fixed part of a row, and
 // what the SM's L2 traffic saves comes back as waits.
 template <typename T, bool GRAD>
@@ -1271,7 +1271,7 @@ bcq_status launch_distill(int n, const void* logits, void* grad, DistillParams p
     const bcq_status st = ensure_dynamic_smem(distill_kernel<T, GRAD>, smem);
     if (st != BCQ_OK) return st;
     // The loss goes from row to row (2048 rows of 50272, fp32: 69 us, a CTA for each 74); the gradient, whose rows take longer than a CTA's
-    // start, has a CTA for each (2048 of 50257, bf16: 94 us, from row to row 97).
+    // start, has a CTA for each (2048 of 50257, bf16: 93 us, from row to row 97).
     const int clusters = GRAD ? n : std::min(n, std::max(1, sm_count() * 3 / p.ctas));
     BCQ_CUDA_TRY(launch_pdl(distill_kernel<T, GRAD>, dim3((unsigned)(clusters * p.ctas)), kDistillThreads + 32, smem, s, (unsigned)p.ctas,
                             (const T*)logits, (T*)grad, p));
