@@ -100,9 +100,6 @@ def _build_tensor_binding():
     if r.returncode != 0:
         raise RuntimeError("g++ failed for binding_torch.cpp:\n" + r.stderr)
     os.replace(out + ".tmp", out)
-    for other in glob.glob(os.path.join(HERE, "_tensor_call*.so")):  # for another torch
-        if other != out:
-            os.remove(other)
 
 
 def _build_cuda(verbose: bool):
@@ -136,6 +133,9 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
             _build_cuda(verbose)
         if binding is not None:
             binding.result()
+    if tensor_call_path():
+        for other in set(glob.glob(os.path.join(HERE, "_tensor_call*.so"))) - {tensor_call_path()}:  # for another torch
+            os.remove(other)
     return LIB
 
 

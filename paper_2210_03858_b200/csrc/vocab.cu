@@ -2,14 +2,14 @@
 // distillation loss against a teacher's top log probabilities with its gradient.
 //
 // With c = log2(e) / T everything is a sum over a row of 2^(c x - b), b = c max x.  The kernels read a row once
-// for its sums (and the gradient's once more, from L2 as far as it is still there): a thread keeps a running maximum and the sums that go with it, and rescales them when a batch of its
-// vectors has a larger one, so no second pass is needed for the sums; the sums of threads, warps and CTAs are joined in
-// a fixed order.  b is the rounded product and is subtracted everywhere (from a target, from an alternative), so its
-// rounding error, which would be that of a probability, drops out (where it would be too large for that, |b| > 2^31, exponents
-// are c (x - max x)).  What bounds them is memory: n vocab sizeof(T) bytes read (and written, for the gradient).  Next to that is the issue of instructions: an element of bf16 costs a
-// conversion, an exponential (16 a cycle and SM: 0.7 of the time its bytes take), half a product and half a sum for each
-// result (two at a time, fma.rn.f32x2), a quarter of a maximum and half a clamp, and with everything that goes with a row
-// 7.6 instructions (9.1 with products and sums one at a time).
+// for its sums (and the gradient's once more, from L2 as far as it is still there): a thread keeps a running maximum and the sums that
+// go with it, and rescales them when a batch of its vectors has a larger one, so no second pass is needed for the sums; the sums of
+// threads, warps and CTAs are joined in a fixed order.  b is the rounded product and is subtracted everywhere (from a target, from an
+// alternative), so its rounding error, which would be that of a probability, drops out (where it would be too large for that,
+// |b| > 2^31, exponents are c (x - max x)).  What bounds them is memory: n vocab sizeof(T) bytes read (and written, for the gradient).
+// Next to that is the issue of instructions: an element of bf16 costs a conversion, an exponential (16 a cycle and SM: 0.7 of the time
+// its bytes take), half a product and half a sum for each result (two at a time, fma.rn.f32x2), a quarter of a maximum and half a
+// clamp, and with everything that goes with a row 7.6 instructions (9.1 with products and sums one at a time).
 // Measured: 2048 rows of 50304 in fp32, no list, 62 us, the rate of a copy; 4096 rows of 50257 in bf16, no list 66 us (95 %),
 // 64 alternatives 103; the loss of 2048 rows of 50272 in fp32 69 us (91 %), of 50257 in bf16 49 us (64 %), with the gradient 93 us
 // (68 %), in fp32 169 us (75 %).
@@ -633,7 +633,7 @@ struct LogprobParams {
     int* top_index;
 };
 
-// (of a logit that is not one of the sum's near base, and where the exponent of 2 may overflow, that of e does not)
+// Relative to a near base with the exponent that the logit has in the sum; otherwise, and where that exponent may overflow, by the quotient.
 __device__ __forceinline__ float log_prob(float x, float m, float log_s, const LogprobParams& p) {
     if (x >= kLowest && is_near(__fmul_rn(m, p.c))) return (rel(x, m, p.c) - log_s) * kLn2;
     return (x - m) * p.inv_t - log_s * kLn2;
@@ -1051,8 +1051,8 @@ __device__ __forceinline__ void zero_row(T* out, int first, int last, int tid, i
 constexpr int kDistillThreads = 256;  // that go through a row; one more warp helps them
 
 // Loss, and with GRAD the gradient.  A CTA (or a cluster of them) goes from row to row for the loss, as far as the grid leaves it
-// several, and has one row for the gradient (the grid has a cluster for each).  Eight warps go through the logits: once for the sums, and for the gradient once more,
-// backwards, which finds the end of the row in L1 and most of the rest in L2 (2048 rows of 50257, bf16: 109 us forwards and past L1,
+// several, and has one row for the gradient (the grid has a cluster for each).  Eight warps go through the logits: once for the sums,
+// and for the gradient once more, backwards, which finds the end of the row in L1 and most of the rest in L2 (2048 rows of 50257, bf16: 109 us forwards and past L1,
 // 97 so).  A ninth has the teacher's list, whose loads depend on one another, and the loss, which is a chain of logarithms in 64 bits:
 // a row ahead of the others and a row behind where there are several, so neither holds up the loads, of which two batches a thread are
 // always on their way.  Barriers: `ready` when a row's tokens are marked, `listed` when the rest of its list is there, `done` when its
