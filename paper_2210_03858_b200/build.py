@@ -5,6 +5,7 @@ Only _tensor_call needs torch (with CUDA): its headers, and the C++ ABI of its l
 too, and it is left out where there is no torch.  The library and _bcq_call are what callers of include/bcq.h need."""
 from __future__ import annotations
 
+import contextlib
 import glob
 import importlib.util
 import os
@@ -135,7 +136,8 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
             binding.result()
     if tensor_call_path():
         for other in set(glob.glob(os.path.join(HERE, "_tensor_call*.so"))) - {tensor_call_path()}:  # for another torch
-            os.remove(other)
+            with contextlib.suppress(FileNotFoundError):  # (another process may have removed it)
+                os.remove(other)
     return LIB
 
 
